@@ -415,6 +415,166 @@ egt_status egt_trigger_depth(double t_ar, double a, double b, const int *cand, c
  * can reach at all on the device; not part of the method. */
 egt_status egt_stream_read(const void *src, size_t bytes, uint32_t *sink, void *stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Beside the products of a verification step (Sec. 3.4: the candidates of a prefix tree pass
+ * the decoder together under a tree mask, and T_score is filtered by the trie).  A batch is
+ * `requests` requests with a few tokens each; the token rows of a request are back to back and
+ * cu_tokens[r] .. cu_tokens[r + 1] are its rows (DEVICE, requests + 1 entries, ascending from
+ * 0).  Rows from cu_tokens[requests] on belong to nobody and are left as they were, and so are the
+ * rows of a request whose two entries are not ascending within the batch.  Lengths, offsets and ids are device
+ * memory and nothing here waits for them: a captured step runs again with other ones.
+ * What a kernel cannot trust it checks before it follows it, and answers with NaN in the rows
+ * concerned, as the products do for a broken row pointer.
+ *
+ * The cache: `blocks` pages of `page` tokens (a power of two), `heads` key heads of `dim` FP16
+ * values.  Element d of head h of the token at place t of page b is at
+ * k[b * k_block + h * k_head + t * k_token + d]; strides in elements, multiples of 8 and not negative, so any
+ * order of pages, heads and tokens will do.  Page p of request r is block_table[r * ld_table
+ * + p], and slot s of the cache is place s % page of block s / page.  Drafted tokens are not in
+ * the cache: attention takes their keys and values from the projection's output, and only the
+ * accepted ones are written. */
+typedef struct {
+  uint16_t *k, *v;
+  int32_t blocks, heads, page, dim;
+  int64_t k_block, k_head, k_token, v_block, v_head, v_token;
+} egt_kv_cache;
+
+/* DEVICE.  Block tables and slot maps from request lengths.  Request r holds lens[r] tokens
+ * in ceil(lens[r] / page) pages of its row of the block table (table_blocks entries); counts[r]
+ * tokens are to follow.  The pages they need beyond those are taken from free_blocks, in the order of the
+ * requests, from entry *free_head on, and entered in the table.  slots[i] (n_slots entries) is the
+ * slot of the i-th new token, all tokens of request 0 first; cu_tokens: the running sum of the counts, held to n_slots;
+ * new_lens[r] = lens[r] + counts[r]; *new_head = *free_head + pages taken.
+ * A request gets no page, keeps its length and has -1 for its slots when its tokens do not fit its row of the table
+ * or end past n_slots, when its length or count is negative (a negative count is 0 in cu_tokens), or when the free pages do not
+ * suffice for it (then no later request that needs a page gets one either).  A slot whose page is not one of
+ * the cache's `blocks` is -1, and so is every entry of slots behind the last token.
+ * lens and new_lens, free_head and new_head must be different buffers: every workgroup
+ * reads the old ones.  1 <= requests <= EGT_MAX_REQUESTS, page a power of two, blocks * page
+ * below 2^31. */
+#define EGT_MAX_REQUESTS 8192
+typedef struct {
+  const int32_t *lens, *counts;       /* [requests]                                          */
+  int32_t *block_table;               /* [requests][ld_table], read and written              */
+  const int32_t *free_blocks;         /* [n_free]                                            */
+  const int32_t *free_head;           /* [1]                                                 */
+  int32_t *slots;                     /* [n_slots]                                           */
+  int32_t *cu_tokens;                 /* [requests + 1]                                      */
+  int32_t *new_lens;                  /* [requests]                                          */
+  int32_t *new_head;                  /* [1]                                                 */
+  int64_t ld_table;
+  int32_t requests, table_blocks, page, blocks, n_free, n_slots;
+} egt_slots_batch;
+egt_status egt_kv_slots(const egt_slots_batch *b, void *stream);
+
+/* DEVICE.  Writes keys and values of new tokens into the cache: row rows[i] (rows == NULL:
+ * row i) of k and v goes to slot slots[i], for i < n.  Entries whose slot is not one of the
+ * cache's (-1: rejected, padding) or whose row is not one of the n_rows are passed over.  Element d of head h of
+ * row i is at k[i * k_row + h * k_head + d]; strides as in the cache.  The slots of a call are
+ * meant to be different; where two are the same, each 16 bytes are one of the two rows'. */
+typedef struct {
+  const uint16_t *k, *v;
+  const int32_t *slots, *rows;        /* [n]; rows may be NULL                               */
+  int64_t k_row, k_head, v_row, v_head;
+  int32_t n, n_rows;
+} egt_append_batch;
+egt_status egt_kv_append(const egt_append_batch *b, const egt_kv_cache *cache, void *stream);
+
+/* DEVICE.  Attention of the drafted tokens of every request, a tree each, over its cached context:
+ *   out[i][h] = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale * q[i][h] . k_j - max),
+ * j over the lens[r] cached tokens of i's request r and those of its drafted tokens whose bit
+ * is set in mask[i]: bit t speaks for the t-th token row of the same request (its own bit
+ * included).  A chain, a tree, a padded row: whatever the bits say; what is masked does
+ * not enter, NaN and infinities included, and a row that sees nothing is zeros (so is one whose
+ * scores are all -infinity).  A token alone is the ordinary decoding step, 64 tokens with the bits of a
+ * chain a piece of a prompt.
+ * Query head h reads key head h / (heads / cache heads).  Up to 64 tokens a request: max_tokens is the
+ * caller's bound, requests with more get NaN.  NaN also where a length is negative or longer than
+ * the table's row, or where a page in use is not one of the cache's.
+ * FP16 in and out; scores, maxima, sums and the weighted sum in FP32, the weights rounded to
+ * FP16 for the matrix cores (relative to the largest, down to 2^-28 of it).
+ * dim: a multiple of 8 up to 256; pointers and strides whole 16 bytes; k and v are read in the
+ * cache's head count.  `out` must not overlap an input.
+ * egt_tree_attention_ws_bytes (HOST): bytes of workspace (DEVICE, 16-byte aligned) that a call
+ * of these requests, tokens, heads, max_tokens, table_blocks and cache sizes needs, never less
+ * than 16; the pointers are not looked at.  The workspace is dead after the call's kernels; calls that share one must not overlap.
+ * EGT_ERR_SHAPE when workspace_bytes is smaller.  Results do not change from run to run. */
+#define EGT_MAX_TREE 64
+typedef struct {
+  const uint16_t *q, *k, *v;          /* element d of head h of row i: q[i * q_row + h * q_head + d] */
+  uint16_t *out;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
+  const int32_t *block_table;         /* [requests][ld_table]                                */
+  const int32_t *lens;                /* [requests]                                          */
+  const int32_t *cu_tokens;           /* [requests + 1]                                      */
+  const uint64_t *mask;               /* [tokens]                                            */
+  int64_t ld_table;
+  int32_t requests, tokens, heads, max_tokens, table_blocks;
+  float scale;
+} egt_tree_batch;
+egt_status egt_tree_attention_ws_bytes(const egt_tree_batch *b, const egt_kv_cache *cache, size_t *bytes);
+egt_status egt_tree_attention(const egt_tree_batch *b, const egt_kv_cache *cache, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* DEVICE.  Low-rank adapters of many requests beside a shared projection, for the M (1..64)
+ * tokens of egt_sparse_gemm_smallm:
+ *   Y[m] = base[m] + scale[a] * B[a] . (A[a] . X[m]),  a = index[m].
+ * A[a]: rank x cols at A + a * a_stride, B[a]: rows x rank at B + a * b_stride (elements),
+ * FP16, rows back to back.  base: M x rows FP16 with row stride ldbase, the projection's
+ * result, NULL for zeros; it may be Y itself (same ldbase and ldy), and must not overlap Y otherwise.  scale: one FP32
+ * per adapter, NULL for ones.  index[m] < 0: no adapter, Y[m] = base[m]; index[m] >= adapters:
+ * NaN.  Any token may have any adapter, and tokens of one adapter read it once.
+ * FP32 sums in a fixed order; A . X[m] goes on as two FP16 numbers that hold 22 of its bits.
+ * cols and rank multiples of 8, rank <= 128, adapters >= 1; X, A, B, a_stride, b_stride and ldx whole 16 bytes.
+ * Workspace as for egt_tree_attention; egt_lora_smallm_ws_bytes is the HOST query. */
+typedef struct {
+  const uint16_t *X, *A, *B, *base;
+  uint16_t *Y;
+  const int32_t *index;               /* [M]                                                 */
+  const float *scale;                 /* [adapters] or NULL                                  */
+  int64_t ldx, ldbase, ldy, a_stride, b_stride;
+  int32_t M, cols, rows, rank, adapters;
+} egt_lora_batch;
+egt_status egt_lora_smallm_ws_bytes(int M, int cols, int rank, size_t *bytes);
+egt_status egt_lora_smallm(const egt_lora_batch *b, void *workspace, size_t workspace_bytes, void *stream);
+
+/* DEVICE.  Penalties for repeated tokens, biases and grammar masks (the trie that filters T_score) on
+ * logits.  For row i of request r and token id t, in this order and in FP32, rounded once:
+ *   x = logits[i][t]
+ *   t written or in the prompt:  x = x > 0 ? x / repetition[r] : x * repetition[r]
+ *   t written c > 0 times:       x = x - frequency[r] * c;  x = x - presence[r]
+ *   t in bias_ids[r]:            x = x + bias[r] of its last entry
+ *   t not allowed:               x = -infinity
+ * Written are history[r][prompt_len[r] .. history_len[r]) and the drafted tokens of the same
+ * request whose bit is set in mask[i] (as in egt_tree_attention: the row's own token and its
+ * ancestors); the prompt is history[r][0 .. prompt_len[r]).  Lengths are held to 0 .. history_width;
+ * ids outside 0 .. vocab - 1 (padding) are passed over.  allowed_row[i] < 0: everything is allowed; otherwise bit t % 32
+ * of allowed[allowed_row[i]][t / 32] decides (n_allowed rows, ld_allowed words apart; an
+ * allowed_row past the last gives NaN in the row).
+ * Any of history (with both lengths), draft (with mask), repetition, frequency, presence, bias_ids
+ * (with bias) and allowed (with allowed_row) may be NULL: that rule is left out, and a prompt_len of NULL is no prompt.
+ * kind: EGT_LOGITS_FP16 or EGT_LOGITS_FP32, of logits and out.  out may be logits itself (same
+ * leading dimension) and must not overlap it otherwise.  Up to 64 tokens a request see each other: bits past a
+ * request's tokens are passed over.  requests <= EGT_MAX_REQUESTS. */
+enum { EGT_LOGITS_FP16 = 0, EGT_LOGITS_FP32 = 1 };
+typedef struct {
+  const void *logits;
+  void *out;
+  const int32_t *cu_tokens;           /* [requests + 1]                                      */
+  const int32_t *history;             /* [requests][history_width], rows ld_history apart    */
+  const int32_t *history_len, *prompt_len;           /* [requests]                           */
+  const int32_t *draft;               /* [tokens]                                            */
+  const uint64_t *mask;               /* [tokens]                                            */
+  const float *repetition, *frequency, *presence;    /* [requests]                           */
+  const int32_t *bias_ids;            /* [requests][n_bias]                                  */
+  const float *bias;                  /* [requests][n_bias]                                  */
+  const uint32_t *allowed;            /* [n_allowed][ld_allowed]                             */
+  const int32_t *allowed_row;         /* [tokens]                                            */
+  int64_t ld_logits, ld_out, ld_history, ld_allowed;
+  int32_t kind, requests, tokens, vocab, history_width, n_bias, n_allowed;
+} egt_rules_batch;
+egt_status egt_logits_rules(const egt_rules_batch *b, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

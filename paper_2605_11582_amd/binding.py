@@ -35,6 +35,8 @@ SYMBOLS = (
     "egt_gemv_stack_plan", "egt_gemv_stack_run", "egt_sparse_gemm_smallm_ws_bytes", "egt_sparse_gemm_smallm_ws",
     "egt_sparse_gemm_smallm_static", "egt_sparse_gemm_smallm_batch",
     "egt_gemm_stack_plan", "egt_gemm_stack_run",
+    "egt_kv_slots", "egt_kv_append", "egt_tree_attention_ws_bytes", "egt_tree_attention",
+    "egt_lora_smallm_ws_bytes", "egt_lora_smallm", "egt_logits_rules",
 )
 
 
@@ -101,10 +103,51 @@ class StackPlan(C.Structure):
             raise AttributeError(f"egt_stack_plan has no field {name}")
 
 
+def _fields(pointers: str, longs: str, ints: str, floats: str = ""):
+    return ([(n, C.c_void_p) for n in pointers.split()] + [(n, C.c_int64) for n in longs.split()] +
+            [(n, C.c_int32) for n in ints.split()] + [(n, C.c_float) for n in floats.split()])
+
+
+class KvCache(C.Structure):
+    """Mirror of `egt_kv_cache`."""
+    _fields_ = _fields("k v", "", "blocks heads page dim") + _fields("", "k_block k_head k_token v_block v_head v_token", "")
+
+
+class SlotsBatch(C.Structure):
+    """Mirror of `egt_slots_batch`."""
+    _fields_ = _fields("lens counts block_table free_blocks free_head slots cu_tokens new_lens new_head", "ld_table",
+                       "requests table_blocks page blocks n_free n_slots")
+
+
+class AppendBatch(C.Structure):
+    """Mirror of `egt_append_batch`."""
+    _fields_ = _fields("k v slots rows", "k_row k_head v_row v_head", "n n_rows")
+
+
+class TreeBatch(C.Structure):
+    """Mirror of `egt_tree_batch`."""
+    _fields_ = (_fields("q k v out", "q_row q_head k_row k_head v_row v_head out_row out_head", "") +
+                _fields("block_table lens cu_tokens mask", "ld_table", "requests tokens heads max_tokens table_blocks", "scale"))
+
+
+class LoraBatch(C.Structure):
+    """Mirror of `egt_lora_batch`."""
+    _fields_ = _fields("X A B base Y index scale", "ldx ldbase ldy a_stride b_stride", "M cols rows rank adapters")
+
+
+class RulesBatch(C.Structure):
+    """Mirror of `egt_rules_batch`."""
+    _fields_ = _fields("logits out cu_tokens history history_len prompt_len draft mask repetition frequency presence bias_ids bias "
+                       "allowed allowed_row", "ld_logits ld_out ld_history ld_allowed",
+                       "kind requests tokens vocab history_width n_bias n_allowed")
+
+
 STACK_ENTRY_BYTES = 160
+MAX_REQUESTS, MAX_TREE = 8192, 64
 
 _lib = None
 _call = None              # the extension module egt_call, bound to the loaded library
+_batches = ("egt_kv_slots", "egt_kv_append", "egt_tree_attention", "egt_tree_attention_ws_bytes", "egt_lora_smallm", "egt_logits_rules")
 _plain = ("egt_sparse_gemv", "egt_sparse_gemm_smallm", "egt_sparse_gemm_smallm_ws", "egt_sparse_gemm_smallm_static", "egt_int4_gemv")
 
 
@@ -148,6 +191,13 @@ def _declare(L: C.CDLL, names=None) -> C.CDLL:
                                        C.c_size_t, C.c_void_p], C.c_int),
         "egt_sparse_gemm_smallm_static": ([C.POINTER(View), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_void_p],
                                           C.c_int),
+        "egt_kv_slots": ([C.POINTER(SlotsBatch), C.c_void_p], C.c_int),
+        "egt_kv_append": ([C.POINTER(AppendBatch), C.POINTER(KvCache), C.c_void_p], C.c_int),
+        "egt_tree_attention_ws_bytes": ([C.POINTER(TreeBatch), C.POINTER(KvCache), C.POINTER(C.c_size_t)], C.c_int),
+        "egt_tree_attention": ([C.POINTER(TreeBatch), C.POINTER(KvCache), C.c_void_p, C.c_size_t, C.c_void_p], C.c_int),
+        "egt_lora_smallm_ws_bytes": ([C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)], C.c_int),
+        "egt_lora_smallm": ([C.POINTER(LoraBatch), C.c_void_p, C.c_size_t, C.c_void_p], C.c_int),
+        "egt_logits_rules": ([C.POINTER(RulesBatch), C.c_void_p], C.c_int),
     }
     for name in names:
         fn = getattr(L, name)                           # AttributeError if the library lacks an entry point
@@ -187,6 +237,7 @@ def _native():
                                "(there is no fallback path)") from e
         egt_call.bind(*[_address(getattr(L, name)) for name in _plain], _check,
                       torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
+        egt_call.bind_batches(*[_address(getattr(L, name)) for name in _batches])
         _call = egt_call
     return _call
 
@@ -702,6 +753,84 @@ def prepared_gemm_stack(items, stream=None):
     call.plans = [t[1] for t in tables]
     call.plan = call.plans[0]
     return call
+
+
+# ------------------------------------------------- beside the products of a verification step
+# egt.h says what each of them computes.  Tensors are checked and marshalled in the extension module (a ValueError names
+# the argument that is wrong); they are all on one device, and without `stream` the call goes to that device's current
+# stream.  The prepared forms marshal once and launch on every call; they keep the tensors alive.
+def kv_slots(lens, counts, block_table, page: int, blocks: int, free_blocks, free_head, slots, cu_tokens, new_lens, new_head, stream=None) -> None:
+    """Block tables and slot maps of requests that grow from lens by counts tokens: int32 device tensors
+    lens, counts, new_lens (R,), block_table (R, W), free_blocks (F,), free_head, new_head (1,), slots (N,),
+    cu_tokens (R + 1,); `page` tokens a page, `blocks` pages in the cache.  Writes block_table (new pages), slots,
+    cu_tokens, new_lens and new_head."""
+    (_call or _native()).kv_slots(False, lens, counts, block_table, page, blocks, free_blocks, free_head, slots, cu_tokens, new_lens, new_head, stream)
+
+
+def prepared_kv_slots(lens, counts, block_table, page: int, blocks: int, free_blocks, free_head, slots, cu_tokens, new_lens, new_head, stream=None):
+    return _native().kv_slots(True, lens, counts, block_table, page, blocks, free_blocks, free_head, slots, cu_tokens, new_lens, new_head, stream)
+
+
+def kv_append(k, v, slots, k_cache, v_cache, rows=None, stream=None) -> None:
+    """Rows of k and v (n, heads, dim) into the slots (int32) of a paged cache (blocks, heads, page, dim), any strides with
+    contiguous dim; entry i writes row rows[i] (without rows: row i); slots outside the cache are passed over."""
+    (_call or _native()).kv_append(False, k, v, slots, k_cache, v_cache, rows, stream)
+
+
+def prepared_kv_append(k, v, slots, k_cache, v_cache, rows=None, stream=None):
+    return _native().kv_append(True, k, v, slots, k_cache, v_cache, rows, stream)
+
+
+def tree_attention_ws_bytes(q, k_cache, block_table, lens, max_tokens: int = MAX_TREE) -> int:
+    """Bytes of device workspace that `tree_attention` needs for tensors of these sizes."""
+    return (_call or _native()).tree_attention_ws_bytes(q, k_cache, block_table, lens, max_tokens)
+
+
+def tree_attention(q, k, v, k_cache, v_cache, block_table, lens, cu_tokens, mask, out, scale: float, max_tokens: int = MAX_TREE,
+                   workspace=None, stream=None) -> None:
+    """Attention of drafted tokens over their requests' cached context and over those of their own request that mask
+    (int64, one bit a token) shows: q, out (N, heads, dim), k, v (N, key heads, dim), caches as for `kv_append`, block_table
+    (R, W), lens (R,), cu_tokens (R + 1,) int32.  `workspace`: a device tensor of tree_attention_ws_bytes bytes."""
+    (_call or _native()).tree_attention(False, q, k, v, k_cache, v_cache, block_table, lens, cu_tokens, mask, out, scale, max_tokens, workspace, stream)
+
+
+def prepared_tree_attention(q, k, v, k_cache, v_cache, block_table, lens, cu_tokens, mask, out, scale: float, max_tokens: int = MAX_TREE,
+                            workspace=None, stream=None):
+    return _native().tree_attention(True, q, k, v, k_cache, v_cache, block_table, lens, cu_tokens, mask, out, scale, max_tokens, workspace, stream)
+
+
+def lora_smallm_ws_bytes(X, A) -> int:
+    """Bytes of device workspace that `lora_smallm` needs for X (M, cols) and A (adapters, rank, cols)."""
+    out = C.c_size_t()
+    _check(lib().egt_lora_smallm_ws_bytes(X.shape[0], X.shape[1], A.shape[1], C.byref(out)))
+    return int(out.value)
+
+
+def lora_smallm(X, A, B, index, Y, workspace, base=None, scale=None, stream=None) -> None:
+    """Y[m] = base[m] + scale[a] * B[a] . (A[a] . X[m]) with a = index[m] (int32; negative: no adapter): X (M, cols),
+    A (adapters, rank, cols), B (adapters, rows, rank), base and Y (M, rows) float16, scale (adapters,) float32.
+    base may be Y: the projection's result with the adapters added."""
+    (_call or _native()).lora_smallm(False, X, A, B, index, Y, workspace, base, scale, stream)
+
+
+def prepared_lora_smallm(X, A, B, index, Y, workspace, base=None, scale=None, stream=None):
+    return _native().lora_smallm(True, X, A, B, index, Y, workspace, base, scale, stream)
+
+
+def logits_rules(logits, out, cu_tokens, history=None, history_len=None, prompt_len=None, draft=None, mask=None, repetition=None, frequency=None,
+                 presence=None, bias_ids=None, bias=None, allowed=None, allowed_row=None, stream=None) -> None:
+    """Penalties, biases and grammar masks on logits (N, vocab), float16 or float32, into out (which may be logits):
+    cu_tokens (R + 1,), history (R, L), history_len, prompt_len (R,), draft (N,) int32, mask (N,) int64, repetition, frequency,
+    presence (R,) float32, bias_ids (R, E) int32 and bias (R, E) float32, allowed (G, ceil(vocab / 32)) int32 words of bits,
+    allowed_row (N,) int32.  What is None is left out."""
+    (_call or _native()).logits_rules(False, logits, out, cu_tokens, history, history_len, prompt_len, draft, mask, repetition, frequency, presence,
+                                      bias_ids, bias, allowed, allowed_row, stream)
+
+
+def prepared_logits_rules(logits, out, cu_tokens, history=None, history_len=None, prompt_len=None, draft=None, mask=None, repetition=None,
+                          frequency=None, presence=None, bias_ids=None, bias=None, allowed=None, allowed_row=None, stream=None):
+    return _native().logits_rules(True, logits, out, cu_tokens, history, history_len, prompt_len, draft, mask, repetition, frequency, presence,
+                                  bias_ids, bias, allowed, allowed_row, stream)
 
 
 def prepared_stream_read(src, nbytes: int, sink, stream=None):

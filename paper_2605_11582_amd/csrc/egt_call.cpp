@@ -9,16 +9,22 @@
 //    (a wrong type, a short buffer, a refused argument) they launch nothing and return False, and
 //    binding.py goes through its own checks, which say what is wrong.  An error of the HIP runtime is
 //    raised from here: the call is not made a second time.
+//  - kv_slots, kv_append, tree_attention, lora_smallm, logits_rules: marshalled here only, plain
+//    and prepared (egt_call_serve.h); they say themselves what is wrong.
 //  - Call: a prepared call, arguments marshalled once; calling it crosses the C ABI.
 //
 // The module is not linked against libegt.so: binding.py hands over the addresses of the
 // entry points of the library it has loaded (bind), whichever build that is.
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <exception>
 #include <memory>
+#include <new>
+#include <string>
 #include <vector>
 
 #include "egt.h"
@@ -35,8 +41,9 @@ typedef int (*gemm_batch_fn)(const void *, const void *, int64_t, const void *, 
 typedef int (*int4_batch_fn)(const void *, const void *, int, int, int, const void *, const void *, int, void *);
 typedef int (*table_fn)(const void *, const void *, void *);
 
-enum Kind { GEMV, READ, GEMM, GEMM_WS, INT4, GEMV_BATCH, GEMM_BATCH, INT4_BATCH, TABLE, KINDS };
-constexpr int N_ARGS[KINDS] = {3, 3, 6, 8, 7, 4, 7, 8, 2};      // without the stream
+// (BATCH, BATCH_WS, TREE: the operators beside the products; kv_append is a TABLE by its signature)
+enum Kind { GEMV, READ, GEMM, GEMM_WS, INT4, GEMV_BATCH, GEMM_BATCH, INT4_BATCH, TABLE, BATCH, BATCH_WS, TREE, KINDS };
+constexpr int N_ARGS[KINDS] = {3, 3, 6, 8, 7, 4, 7, 8, 2, 1, 3, 4};      // without the stream
 
 struct Thunk {
   Kind kind;
@@ -54,6 +61,9 @@ struct Thunk {
       case GEMV_BATCH: return ((gemv_batch_fn)fn)(p(0), p(1), p(2), i(3), s);
       case GEMM_BATCH: return ((gemm_batch_fn)fn)(p(0), p(1), a[2], p(3), a[4], i(5), i(6), s);
       case INT4_BATCH: return ((int4_batch_fn)fn)(p(0), p(1), i(2), i(3), i(4), p(5), p(6), i(7), s);
+      case BATCH: return ((int (*)(const void *, void *))fn)(p(0), s);
+      case BATCH_WS: return ((int (*)(const void *, void *, size_t, void *))fn)(p(0), p(1), (size_t)a[2], s);
+      case TREE: return ((int (*)(const void *, const void *, void *, size_t, void *))fn)(p(0), p(1), p(2), (size_t)a[3], s);
       default: return ((table_fn)fn)(p(0), p(1), s);
     }
   }
@@ -337,11 +347,20 @@ PyObject *bind(PyObject *, PyObject *args) {
   Py_RETURN_NONE;
 }
 
+#include "egt_call_serve.h"
+
 PyMethodDef methods[] = {
     {"bind", bind, METH_VARARGS, nullptr},
     {"sparse_gemv", (PyCFunction)(void (*)(void))guarded<sparse_gemv>, METH_FASTCALL, nullptr},
     {"sparse_gemm_smallm", (PyCFunction)(void (*)(void))guarded<sparse_gemm_smallm>, METH_FASTCALL, nullptr},
     {"int4_gemv", (PyCFunction)(void (*)(void))guarded<int4_gemv>, METH_FASTCALL, nullptr},
+    {"bind_batches", bind_batches, METH_VARARGS, nullptr},
+    {"kv_slots", (PyCFunction)(void (*)(void))batch_call<Slots>, METH_FASTCALL, nullptr},
+    {"kv_append", (PyCFunction)(void (*)(void))batch_call<Append>, METH_FASTCALL, nullptr},
+    {"tree_attention", (PyCFunction)(void (*)(void))batch_call<Tree>, METH_FASTCALL, nullptr},
+    {"tree_attention_ws_bytes", (PyCFunction)(void (*)(void))tree_bytes, METH_FASTCALL, nullptr},
+    {"lora_smallm", (PyCFunction)(void (*)(void))batch_call<Lora>, METH_FASTCALL, nullptr},
+    {"logits_rules", (PyCFunction)(void (*)(void))batch_call<Rules>, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "egt_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 // A copy of a call, shallow or deep, is the call itself, as for a function: its pointers are those of its buffers.
@@ -379,7 +398,7 @@ PyMODINIT_FUNC PyInit_egt_call(void) {
       {&S.stream_ptr, "stream_ptr"}, {&S.value, "value"}};
   for (const auto &n : names)
     if (!(*n.at = PyUnicode_InternFromString(n.name))) return nullptr;
-  const char *kinds[KINDS] = {"GEMV", "READ", "GEMM", "GEMM_WS", "INT4", "GEMV_BATCH", "GEMM_BATCH", "INT4_BATCH", "TABLE"};
+  const char *kinds[KINDS] = {"GEMV", "READ", "GEMM", "GEMM_WS", "INT4", "GEMV_BATCH", "GEMM_BATCH", "INT4_BATCH", "TABLE", "BATCH", "BATCH_WS", "TREE"};
   for (int k = 0; k < KINDS; ++k)
     if (PyModule_AddIntConstant(m, kinds[k], k) < 0) return nullptr;
   Py_INCREF(&CallType);

@@ -1,0 +1,174 @@
+// The cache of a verification step: block tables and slot maps from request lengths, and the rows of new
+// tokens into their slots.
+#include "egt_serve.h"
+
+#include <algorithm>
+
+namespace egt {
+namespace {
+
+constexpr int SLOT_THREADS = 256;
+
+// Sum of `v` over the threads before this one.  `part`: one word a wave; all threads of the workgroup call it.
+__device__ __forceinline__ int64_t sum_before(int64_t v, int64_t *part) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t s = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t t = __shfl_up(s, o, 64);
+    if (lane >= o) s += t;
+  }
+  if (lane == 63) part[wave] = s;
+  __syncthreads();
+  int64_t before = s - v;
+  for (int w = 0; w < wave; ++w) before += part[w];
+  __syncthreads();                                    // (part is used again)
+  return before;
+}
+
+// Two running sums over the requests - tokens, then pages - decide everything, and a few thousand lengths are 16 KB: every
+// workgroup computes both for itself (each thread a run of requests, then one scan over the threads) and keeps them in LDS, so
+// that the token slots, which are the bytes, are written by the whole chip without a second launch and without one workgroup
+// waiting for another.  What binds it is that chain: two loads, two scans, a search, a page number.
+__global__ __launch_bounds__(SLOT_THREADS) void k_kv_slots(egt_slots_batch b, int shift) {
+  extern __shared__ int32_t lds[];
+  __shared__ int64_t part[SLOT_THREADS / 64];
+  const int n = b.requests, tid = threadIdx.x;
+  int32_t *cu = lds, *first = lds + n + 1;            // first token; first free page (-1: the request gets nothing)
+  const int per = (n + SLOT_THREADS - 1) / SLOT_THREADS;
+  const int r0 = min(tid * per, n), r1 = min(r0 + per, n);
+  int64_t tokens = 0;
+  for (int r = r0; r < r1; ++r) tokens += max(b.counts[r], 0);
+  int64_t at = sum_before(tokens, part), pages = 0;
+  for (int r = r0; r < r1; ++r) {
+    const int64_t len = b.lens[r], c = b.counts[r], end = at + max(c, (int64_t)0);
+    const bool room = len >= 0 && c >= 0 && len + c <= (int64_t)b.table_blocks << shift && end <= b.n_slots;
+    const int64_t up = (1 << shift) - 1, need = room ? ((len + c + up) >> shift) - ((len + up) >> shift) : 0;
+    cu[r] = (int32_t)min(at, (int64_t)b.n_slots);
+    first[r] = room ? (int32_t)need : -1;
+    at = end;
+    pages += need;
+  }
+  if (r0 < r1 && r1 == n) cu[n] = (int32_t)min(at, (int64_t)b.n_slots);
+  const int head = *b.free_head;
+  const int64_t left = head >= 0 ? max((int64_t)b.n_free - head, (int64_t)0) : 0;
+  int64_t start = sum_before(pages, part), top = 0;
+  for (int r = r0; r < r1; ++r) {
+    const int need = first[r];
+    if (need <= 0) continue;                          // (no page needed: kept, at 0; refused already: -1)
+    start += need;
+    first[r] = start <= left ? (int32_t)(start - need) : -1;
+    if (start <= left) top = start;
+  }
+  __syncthreads();
+
+  if (blockIdx.x == 0) {
+    for (int r = tid; r <= n; r += SLOT_THREADS) b.cu_tokens[r] = cu[r];
+    for (int r = tid; r < n; r += SLOT_THREADS) b.new_lens[r] = b.lens[r] + (first[r] >= 0 ? b.counts[r] : 0);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
+    if ((tid & 63) == 0) part[tid >> 6] = top;
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < SLOT_THREADS / 64; ++w) top = max(top, part[w]);
+      *b.new_head = head + (int32_t)top;
+    }
+  }
+  // the pages that are taken: a wave a request
+  const int waves = gridDim.x * (SLOT_THREADS / 64);
+  for (int r = blockIdx.x * (SLOT_THREADS / 64) + (tid >> 6); r < n; r += waves) {
+    if (first[r] < 0) continue;
+    const int64_t up = (1 << shift) - 1, len = b.lens[r];
+    const int have = (int)((len + up) >> shift), all = (int)((len + b.counts[r] + up) >> shift);
+    for (int p = have + (tid & 63); p < all; p += 64) b.block_table[(int64_t)r * b.ld_table + p] = b.free_blocks[head + first[r] + p - have];
+  }
+  // the slots: four in a row a thread
+  const bool whole = ((uintptr_t)b.slots & 15u) == 0;
+  for (int64_t i0 = 4 * ((int64_t)blockIdx.x * SLOT_THREADS + tid); i0 < b.n_slots; i0 += 4 * (int64_t)SLOT_THREADS * gridDim.x) {
+    int r = 0;                                        // the last request that starts at i0 or before (n: no request's)
+    for (int lo = 0, hi = n + 1; lo < hi;) {
+      const int mid = (lo + hi) >> 1;
+      if (cu[mid] <= i0) { r = mid; lo = mid + 1; } else { hi = mid; }
+    }
+    int32_t s[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t i = i0 + j;
+      while (r < n && i >= cu[r + 1]) ++r;
+      s[j] = -1;
+      if (r < n && first[r] >= 0) {
+        const int len = b.lens[r], pos = len + (int)(i - cu[r]), p = pos >> shift, have = (int)(((int64_t)len + (1 << shift) - 1) >> shift);
+        const int block = p < have ? b.block_table[(int64_t)r * b.ld_table + p] : b.free_blocks[head + first[r] + p - have];
+        if (block >= 0 && block < b.blocks) s[j] = (block << shift) + (pos & ((1 << shift) - 1));
+      }
+    }
+    if (whole && i0 + 4 <= b.n_slots) {
+      *(int4 *)(b.slots + i0) = int4{s[0], s[1], s[2], s[3]};
+    } else {
+      for (int j = 0; j < 4 && i0 + j < b.n_slots; ++j) b.slots[i0 + j] = s[j];
+    }
+  }
+}
+
+// A copy: bound by memory, or, for the tokens of a step, by the latency of a slot number and a row behind it.  2^tshift threads
+// walk a token's 16-byte pieces, keys and values together (two requests in flight a piece); short rows share a workgroup.
+__global__ __launch_bounds__(256) void k_kv_append(egt_append_batch b, egt_kv_cache c, int shift, int tshift) {
+  const int t = threadIdx.x & ((1 << tshift) - 1);
+  const int64_t i = ((int64_t)blockIdx.x << (8 - tshift)) + (threadIdx.x >> tshift);
+  if (i >= b.n) return;
+  const int slot = b.slots[i], row = b.rows ? b.rows[i] : (int)i;
+  if (slot < 0 || (slot >> shift) >= c.blocks || row < 0 || row >= b.n_rows) return;
+  const int64_t block = slot >> shift, place = slot & ((1 << shift) - 1);
+  const uint16_t *ks = b.k + row * b.k_row, *vs = b.v + row * b.v_row;
+  uint16_t *kd = c.k + block * c.k_block + place * c.k_token, *vd = c.v + block * c.v_block + place * c.v_token;
+  const int per = c.dim / 8;
+  for (int p = t; p < c.heads * per; p += 1 << tshift) {
+    const int h = p / per, d = 8 * (p - h * per);
+    const uint4 kk = *(const uint4 *)(ks + h * b.k_head + d), vv = *(const uint4 *)(vs + h * b.v_head + d);
+    *(uint4 *)(kd + h * c.k_head + d) = kk;
+    *(uint4 *)(vd + h * c.v_head + d) = vv;
+  }
+}
+
+inline bool whole4(const void *p) { return ((uintptr_t)p & 3u) == 0; }
+
+}  // namespace
+}  // namespace egt
+
+extern "C" {
+
+egt_status egt_kv_slots(const egt_slots_batch *b, void *stream) {
+  if (!b) return EGT_ERR_NULL;
+  if (b->requests < 1 || b->table_blocks < 0 || b->ld_table < b->table_blocks || b->page < 1 || (b->page & (b->page - 1)) != 0 || b->blocks < 0 ||
+      (int64_t)b->blocks * b->page >= (1ll << 31) || (int64_t)b->table_blocks * b->page >= (1ll << 31) || b->n_free < 0 || b->n_slots < 0)
+    return EGT_ERR_SHAPE;
+  if (b->requests > EGT_MAX_REQUESTS) return EGT_ERR_UNSUPPORTED;
+  if (!b->lens || !b->counts || (b->table_blocks && !b->block_table) || (b->n_free && !b->free_blocks) || !b->free_head || (b->n_slots && !b->slots) ||
+      !b->cu_tokens || !b->new_lens || !b->new_head)
+    return EGT_ERR_NULL;
+  for (const void *p : {(const void *)b->lens, (const void *)b->counts, (const void *)b->block_table, (const void *)b->free_blocks, (const void *)b->free_head,
+                        (const void *)b->slots, (const void *)b->cu_tokens, (const void *)b->new_lens, (const void *)b->new_head})
+    if (!egt::whole4(p)) return EGT_ERR_BUFFER;
+  if (b->lens == b->new_lens || b->counts == b->new_lens || b->free_head == b->new_head) return EGT_ERR_BUFFER;
+  const int64_t want = ((int64_t)b->n_slots + 4 * egt::SLOT_THREADS - 1) / (4 * egt::SLOT_THREADS);
+  const dim3 grid((unsigned)std::min<int64_t>(std::max<int64_t>(want, 1), 512)), block(egt::SLOT_THREADS);
+  return egt::answer(egt::launch(egt::k_kv_slots, grid, block, 4 * (size_t)(2 * b->requests + 1), (hipStream_t)stream, *b, egt::log2_of(b->page)));
+}
+
+egt_status egt_kv_append(const egt_append_batch *b, const egt_kv_cache *cache, void *stream) {
+  if (!b) return EGT_ERR_NULL;
+  const egt_status st = egt::check_cache(cache, true);
+  if (st != EGT_OK) return st;
+  if (b->n < 0 || b->n_rows < 0) return EGT_ERR_SHAPE;
+  if (b->n == 0 || b->n_rows == 0 || cache->blocks == 0) return EGT_OK;          // nothing to write
+  if (!b->k || !b->v || !b->slots) return EGT_ERR_NULL;
+  if (!egt::whole16(b->k) || !egt::whole16(b->v) || !egt::whole8(b->k_row, b->k_head, b->v_row, b->v_head) || !egt::whole4(b->slots) || !egt::whole4(b->rows))
+    return EGT_ERR_BUFFER;
+  const int pieces = cache->heads * (cache->dim / 8);
+  int tshift = 2;
+  while (tshift < 8 && (1 << tshift) < pieces) ++tshift;
+  const int64_t groups = ((int64_t)b->n + (256 >> tshift) - 1) >> (8 - tshift);
+  return egt::answer(egt::launch(egt::k_kv_append, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)stream, *b, *cache, egt::log2_of(cache->page), tshift));
+}
+
+}  // extern "C"

@@ -1,0 +1,206 @@
+"""The operators beside the products without a GPU: what they refuse, what their structures look like, their references."""
+import ctypes as C
+import os
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_11582_amd import binding as egt
+import serve_reference as R
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 1 << 20                # a made-up address: nothing follows it on the host
+NULL, SHAPE, BUFFER, UNSUPPORTED = 1, 2, 5, 6
+MIRRORS = {"egt_kv_cache": egt.KvCache, "egt_slots_batch": egt.SlotsBatch, "egt_append_batch": egt.AppendBatch, "egt_tree_batch": egt.TreeBatch,
+           "egt_lora_batch": egt.LoraBatch, "egt_rules_batch": egt.RulesBatch}
+
+
+def test_structures_are_those_of_the_header(tmp_path):
+    cc = shutil.which("gcc")
+    if not cc:
+        pytest.skip("no host compiler")
+    lines = []
+    for name, mirror in MIRRORS.items():
+        lines.append(f'printf("%zu\\n", sizeof({name}));')
+        lines += [f'printf("%zu\\n", offsetof({name}, {f}));' for f, _ in mirror._fields_]
+    (tmp_path / "s.c").write_text('#include <stdio.h>\n#include "egt.h"\nint main(void) {' + "\n".join(lines) + "return 0; }\n")
+    subprocess.run([cc, "-I" + os.path.join(ROOT, "include"), str(tmp_path / "s.c"), "-o", str(tmp_path / "s")], check=True)
+    got = [int(v) for v in subprocess.run([str(tmp_path / "s")], capture_output=True, text=True, check=True).stdout.split()]
+    want = []
+    for mirror in MIRRORS.values():
+        want += [C.sizeof(mirror)] + [getattr(mirror, f).offset for f, _ in mirror._fields_]
+    assert got == want
+
+
+def cache(**change):
+    c = dict(k=P, v=P, blocks=8, heads=2, page=16, dim=64, k_block=2048, k_head=1024, k_token=64, v_block=2048, v_head=1024, v_token=64)
+    return egt.KvCache(**{**c, **change})
+
+
+def slots(**change):
+    b = dict(lens=P, counts=P, block_table=P, free_blocks=P, free_head=P, slots=P, cu_tokens=P, new_lens=2 * P, new_head=2 * P, ld_table=4, requests=3,
+             table_blocks=4, page=16, blocks=8, n_free=5, n_slots=7)
+    return egt.SlotsBatch(**{**b, **change})
+
+
+def append(**change):
+    return egt.AppendBatch(**{**dict(k=P, v=P, slots=P, k_row=128, k_head=64, v_row=128, v_head=64, n=4, n_rows=4), **change})
+
+
+def tree(**change):
+    b = dict(q=P, k=P, v=P, out=P, q_row=256, q_head=64, k_row=128, k_head=64, v_row=128, v_head=64, out_row=256, out_head=64, block_table=P, lens=P,
+             cu_tokens=P, mask=P, ld_table=4, requests=3, tokens=9, heads=4, max_tokens=5, table_blocks=4, scale=0.125)
+    return egt.TreeBatch(**{**b, **change})
+
+
+def lora(**change):
+    b = dict(X=P, A=P, B=P, base=P, Y=P, index=P, scale=P, ldx=64, ldbase=100, ldy=100, a_stride=512, b_stride=800, M=4, cols=64, rows=100, rank=8, adapters=3)
+    return egt.LoraBatch(**{**b, **change})
+
+
+def rules(**change):
+    b = dict(logits=P, out=P, cu_tokens=P, history=P, history_len=P, draft=P, mask=P, bias_ids=P, bias=P, allowed=P, allowed_row=P, ld_logits=100,
+             ld_out=100, ld_history=10, ld_allowed=4, kind=0, requests=2, tokens=5, vocab=100, history_width=10, n_bias=3, n_allowed=2)
+    return egt.RulesBatch(**{**b, **change})
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(requests=0), SHAPE), (dict(requests=egt.MAX_REQUESTS + 1), UNSUPPORTED), (dict(page=12), SHAPE), (dict(page=0), SHAPE), (dict(ld_table=3), SHAPE),
+    (dict(table_blocks=-1), SHAPE), (dict(n_slots=-1), SHAPE), (dict(n_free=-1), SHAPE), (dict(blocks=1 << 27), SHAPE), (dict(lens=None), NULL),
+    (dict(counts=None), NULL), (dict(block_table=None), NULL), (dict(free_blocks=None), NULL), (dict(free_head=None), NULL), (dict(slots=None), NULL),
+    (dict(cu_tokens=None), NULL), (dict(new_lens=None), NULL), (dict(new_head=None), NULL), (dict(new_lens=P), BUFFER), (dict(new_head=P), BUFFER),
+    (dict(slots=P + 2), BUFFER), (dict(lens=P + 1), BUFFER)])
+def test_kv_slots_refuses(change, status):
+    assert egt.lib().egt_kv_slots(C.byref(slots(**change)), None) == status
+
+
+@pytest.mark.parametrize("change,cached,status", [
+    (dict(n=-1), {}, SHAPE), (dict(n_rows=-1), {}, SHAPE), (dict(k=None), {}, NULL), (dict(v=None), {}, NULL), (dict(slots=None), {}, NULL), (dict(k=P + 8), {}, BUFFER),
+    (dict(k_row=4), {}, BUFFER), (dict(v_head=-64), {}, BUFFER), (dict(slots=P + 2), {}, BUFFER), ({}, dict(page=6), SHAPE), ({}, dict(dim=12), SHAPE),
+    ({}, dict(dim=264), SHAPE), ({}, dict(heads=0), SHAPE), ({}, dict(blocks=-1), SHAPE), ({}, dict(blocks=1 << 27), SHAPE), ({}, dict(k=None), NULL),
+    ({}, dict(v=None), NULL), ({}, dict(k_token=68), BUFFER), ({}, dict(v=P + 2), BUFFER), ({}, dict(v_block=-2048), BUFFER),
+    (dict(n=0, k=None), {}, 0), (dict(n_rows=0, k=None), {}, 0), (dict(k=None), dict(blocks=0, k=None, v=None), 0)])
+def test_kv_append_refuses(change, cached, status):
+    assert egt.lib().egt_kv_append(C.byref(append(**change)), C.byref(cache(**cached)), None) == status
+
+
+@pytest.mark.parametrize("change,cached,status", [
+    (dict(heads=3), {}, SHAPE), (dict(heads=0), {}, SHAPE), (dict(max_tokens=0), {}, SHAPE), (dict(max_tokens=65), {}, SHAPE), (dict(requests=-1), {}, SHAPE),
+    (dict(tokens=-1), {}, SHAPE), (dict(table_blocks=-1), {}, SHAPE), (dict(ld_table=3), {}, SHAPE), (dict(scale=float("nan")), {}, SHAPE),
+    (dict(table_blocks=1 << 28, ld_table=1 << 28), {}, SHAPE), (dict(requests=egt.MAX_REQUESTS + 1), {}, UNSUPPORTED), ({}, dict(dim=20), SHAPE),
+    ({}, dict(page=24), SHAPE), (dict(q=None), {}, NULL), (dict(k=None), {}, NULL), (dict(v=None), {}, NULL), (dict(out=None), {}, NULL), (dict(lens=None), {}, NULL),
+    (dict(cu_tokens=None), {}, NULL), (dict(mask=None), {}, NULL), (dict(block_table=None), {}, NULL), (dict(q=P + 8), {}, BUFFER), (dict(out=P + 4), {}, BUFFER),
+    (dict(q_row=260), {}, BUFFER), (dict(out_head=60), {}, BUFFER), (dict(mask=P + 4), {}, BUFFER), (dict(lens=P + 2), {}, BUFFER), ({}, dict(k_token=60), BUFFER),
+    (dict(requests=0, q=None), {}, 0), (dict(tokens=0, q=None), {}, 0)])
+def test_tree_attention_refuses(change, cached, status):
+    L, b, c = egt.lib(), tree(**change), cache(**cached)
+    assert L.egt_tree_attention(C.byref(b), C.byref(c), P, 1 << 30, None) == status
+
+
+def test_tree_attention_workspace():
+    L, n = egt.lib(), C.c_size_t()
+    for change in ({}, dict(max_tokens=64, heads=64), dict(table_blocks=1 << 20, requests=1), dict(requests=64, table_blocks=4096)):
+        b, c = tree(**{**change, "q": None, "k": None, "out": None}), cache(k=None, v=None)
+        assert L.egt_tree_attention_ws_bytes(C.byref(b), C.byref(c), C.byref(n)) == 0 and n.value >= 16 and n.value % 16 == 0
+        b, c, need = tree(**{**change, "ld_table": 1 << 20}), cache(), n.value
+        assert L.egt_tree_attention(C.byref(b), C.byref(c), None, need, None) == NULL
+        assert L.egt_tree_attention(C.byref(b), C.byref(c), P, need - 1, None) == SHAPE
+        assert L.egt_tree_attention(C.byref(b), C.byref(c), P + 8, need, None) == BUFFER
+    assert L.egt_tree_attention_ws_bytes(C.byref(tree()), C.byref(cache()), None) == NULL
+    assert L.egt_tree_attention_ws_bytes(C.byref(tree(max_tokens=65)), C.byref(cache()), C.byref(n)) == SHAPE
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(M=0), SHAPE), (dict(M=65), SHAPE), (dict(cols=60), SHAPE), (dict(rank=12), SHAPE), (dict(rank=0), SHAPE), (dict(rank=136), UNSUPPORTED),
+    (dict(rows=-1), SHAPE), (dict(adapters=0), SHAPE), (dict(ldx=56), SHAPE), (dict(ldy=99), SHAPE), (dict(ldbase=99), SHAPE), (dict(ldbase=104), SHAPE),
+    (dict(a_stride=-8), SHAPE), (dict(X=None), NULL), (dict(A=None), NULL), (dict(B=None), NULL), (dict(Y=None), NULL), (dict(index=None), NULL),
+    (dict(X=P + 8), BUFFER), (dict(A=P + 2), BUFFER), (dict(ldx=68), BUFFER), (dict(b_stride=804), BUFFER), (dict(index=P + 1), BUFFER), (dict(rows=0, X=None), 0)])
+def test_lora_smallm_refuses(change, status):
+    b = lora(**change)
+    assert egt.lib().egt_lora_smallm(C.byref(b), P, 1 << 30, None) == status
+
+
+def test_lora_smallm_workspace():
+    L, n = egt.lib(), C.c_size_t()
+    for M, cols, rank in ((1, 8, 8), (64, 4096, 16), (64, 16384, 128)):
+        assert L.egt_lora_smallm_ws_bytes(M, cols, rank, C.byref(n)) == 0 and n.value >= 16
+        b = lora(M=M, cols=cols, ldx=cols, rank=rank)
+        assert L.egt_lora_smallm(C.byref(b), P, n.value - 1, None) == SHAPE
+        assert L.egt_lora_smallm(C.byref(b), None, n.value, None) == NULL
+    assert L.egt_lora_smallm_ws_bytes(65, 8, 8, C.byref(n)) == SHAPE and L.egt_lora_smallm_ws_bytes(1, 8, 8, None) == NULL
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(kind=2), SHAPE), (dict(requests=-1), SHAPE), (dict(tokens=-1), SHAPE), (dict(vocab=-1), SHAPE), (dict(ld_logits=99), SHAPE), (dict(ld_out=99), SHAPE),
+    (dict(ld_out=104), SHAPE), (dict(ld_history=9), SHAPE), (dict(history_width=-1), SHAPE), (dict(ld_allowed=3), SHAPE), (dict(n_bias=-1), SHAPE),
+    (dict(requests=egt.MAX_REQUESTS + 1), UNSUPPORTED), (dict(logits=None), NULL), (dict(out=None), NULL), (dict(cu_tokens=None), NULL), (dict(history_len=None), NULL),
+    (dict(mask=None), NULL), (dict(bias=None), NULL), (dict(allowed_row=None), NULL), (dict(logits=P + 1, out=2 * P), BUFFER), (dict(kind=1, out=2 * P + 2), BUFFER),
+    (dict(mask=P + 4), BUFFER), (dict(history=P + 2), BUFFER), (dict(requests=0, logits=None), 0), (dict(tokens=0, logits=None), 0), (dict(vocab=0, logits=None), 0)])
+def test_logits_rules_refuses(change, status):
+    assert egt.lib().egt_logits_rules(C.byref(rules(**change)), None) == status
+
+
+def test_the_binding_names_what_is_wrong():
+    i, h = torch.zeros(4, dtype=torch.int32), torch.zeros((4, 2, 8), dtype=torch.float16)
+    with pytest.raises(ValueError, match="lens: expected a device tensor"):
+        egt.kv_slots(i, i, i.view(4, 1), 16, 4, i, i[:1], i, i, i, i[:1])
+    with pytest.raises(ValueError, match="k: expected a device tensor"):
+        egt.kv_append(h, h, i, h, h)
+    with pytest.raises(ValueError, match="q: expected a device tensor"):
+        egt.tree_attention(h, h, h, h, h, i, i, i, i, h, 1.0)
+    with pytest.raises(ValueError, match="X: expected a device tensor"):
+        egt.lora_smallm(h[0], h, h, i, h[0], None)
+    with pytest.raises(ValueError, match="logits: expected a device tensor"):
+        egt.logits_rules(h[0], h[0], i)
+    with pytest.raises(ValueError, match="logits"):
+        egt.prepared_logits_rules(None, h[0], i)
+    with pytest.raises(TypeError):
+        egt._native().kv_slots(False, i)
+
+
+def test_tensors_without_memory_are_refused():
+    from torch._subclasses.fake_tensor import FakeTensorMode
+
+    def body(t, i):
+        for call in (lambda: egt.kv_append(t, t, i, t[None], t[None]), lambda: egt.logits_rules(t[0], t[0], i), lambda: egt.prepared_logits_rules(t[0], t[0], i)):
+            with pytest.raises(ValueError):
+                call()
+        return t
+    with FakeTensorMode():
+        torch.vmap(body)(torch.empty((3, 4, 8, 64), dtype=torch.float16, device="cuda"), torch.empty((3, 4), dtype=torch.int32, device="cuda"))
+
+
+# ---------------------------------------------------------------- the references themselves, on numbers worked out by hand
+def test_reference_of_slots():
+    lens, counts = np.array([3, 0, 4]), np.array([2, 1, 4])
+    table = np.array([[7, -1], [-1, -1], [5, -1]], dtype=np.int32)
+    slots_, cu, new, head, table = R.kv_slots(lens, counts, table, 4, 10, np.array([9, 2, 3, 4]), 1, 8)
+    # request 0 fills place 3 of page 7, then takes page 2; request 1 takes 3; request 2, whose page is full, takes 4
+    assert slots_.tolist() == [31, 8, 12, 16, 17, 18, 19, -1] and cu.tolist() == [0, 2, 3, 7] and new.tolist() == [5, 1, 8] and head.tolist() == [4]
+    assert table.tolist() == [[7, 2], [3, -1], [5, 4]]
+    slots_, _, new, head, _ = R.kv_slots(lens, counts, np.array([[7, -1], [-1, -1], [5, -1]], dtype=np.int32), 4, 10, np.array([9, 2]), 1, 8)
+    assert slots_.tolist() == [31, 8, -1, -1, -1, -1, -1, -1] and new.tolist() == [5, 0, 4] and head.tolist() == [2]
+
+
+def test_reference_of_attention():
+    q = np.array([[[1.0, 0.0]], [[0.0, 1.0]]])
+    k = np.array([[[0.0, 0.0]], [[0.0, np.log(3.0)]]])
+    v = np.array([[[1.0, 2.0]], [[5.0, 6.0]]])
+    kc = np.array([[[[np.log(2.0), 0.0]]]])
+    vc = np.array([[[[4.0, 8.0]]]])
+    out, _ = R.tree_attention(q, k, v, kc, vc, np.array([[0]]), np.array([1]), [0, 2], np.array([1, 2], np.uint64), 1.0)
+    # token 0: weights 2 (cached) and 1 (itself); token 1: weights 1 (cached) and 3 (itself)
+    assert np.allclose(out[0, 0], [3.0, 6.0]) and np.allclose(out[1, 0], [(4 + 15) / 4, (8 + 18) / 4])
+    out, _ = R.tree_attention(q, k, v, kc, vc, np.array([[0]]), np.array([0]), [0, 2], np.array([0, 1], np.uint64), 1.0)
+    assert np.all(out[0] == 0) and np.allclose(out[1, 0], [1.0, 2.0])
+
+
+def test_reference_of_rules():
+    x = np.array([[2.0, -2.0, 1.0, 4.0, 0.5]])
+    out, _ = R.rules(x, [0, 1], False, history=np.array([[1, 0, 0, 9, 2]]), history_len=np.array([4]), prompt_len=np.array([1]), draft=np.array([3]),
+                     mask=np.array([1], np.uint64), repetition=np.array([2.0]), frequency=np.array([0.25]), presence=np.array([0.5]),
+                     bias_ids=np.array([[4, 3, 4]]), bias=np.array([[1.0, -1.0, 3.0]]), allowed=np.array([[0b11011]], np.int32), allowed_row=np.array([0]))
+    assert out.tolist() == [[2 / 2 - 0.5 - 0.5, -4.0, -np.inf, 4 / 2 - 0.25 - 0.5 - 1, 3.5]]
