@@ -1,82 +1,427 @@
 // Attention of drafted trees over a paged cache.
+//
+// Of one request and one key head, all query rows - its drafted tokens times the query heads that share the key head - meet
+// the same keys: the cache is read once for all of them.  A workgroup has four waves, WR of them side by side over the rows
+// (16 NR rows each) and 4 / WR over the keys; a wave takes 32 keys at a time, and the grid cuts the keys into `splits` spans
+// where requests and heads alone do not fill the chip.  Nothing in the loop is shared between waves, so there is no barrier in it:
+//
+//   S^T = K Q^T    K straight from the cache into the A operand (a lane: one key, 8 values of d), Q^T held in registers.
+//                  Lane (g, n) gets scores of row n and keys 4 g .. 4 g + 3 of either half of the 32.
+//   p = exp2       against a reference per row that is raised only where a score passes it by 2^5: sums and O are rescaled
+//                  rarely, and the maximum is joined over lanes only then.
+//   O^T += V^T P^T the scores' layout is the B operand's if the 32 keys are counted 4 g + i, 16 + 4 g + i, so p goes on in its lane; V^T comes
+//                  out of LDS (a wave's own 32 keys) by the transposing read.
+//
+// What bounds it: the cache's bytes while a key head has up to about 128 rows; above that matrix and exponential work.
+#include "egt_mfma_common.h"
 #include "egt_serve.h"
+
+#include <algorithm>
 
 namespace egt {
 namespace {
 
-// One workgroup of four waves a (token, head): a wave takes 64 keys at a time, a lane one of them.
-__global__ __launch_bounds__(256) void k_tree_simple(egt_tree_batch b, egt_kv_cache c, int shift) {
-  __shared__ float q[256], w[4][64], o[4][256], ml[4][2];
-  const int r = blockIdx.z, h = blockIdx.y, kh = h / (b.heads / c.heads), tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int t0 = b.cu_tokens[r], t1 = b.cu_tokens[r + 1], i = t0 + blockIdx.x;
-  if (t0 < 0 || t1 > b.tokens || i >= t1) return;
-  __half *out = (__half *)b.out + i * b.out_row + h * b.out_head;
-  const int len = b.lens[r], n = t1 - t0;
-  bool bad = n > b.max_tokens || len < 0 || len > (int64_t)b.table_blocks << shift;
-  if (bad) {
-    if (tid < c.dim) out[tid] = __float2half(__builtin_nanf(""));
-    if (n > b.max_tokens && blockIdx.x == 0)          // (the rows that the grid does not reach)
-      for (int j = b.max_tokens; j < n; ++j)
-        if (tid < c.dim) ((__half *)b.out + (int64_t)(t0 + j) * b.out_row + h * b.out_head)[tid] = __float2half(__builtin_nanf(""));
+constexpr int TILE = 32;             // keys a wave takes at a time
+// p is held as 2^SHIFT p against its reference, and may pass it by 2^SLACK: 2^15 at most in FP16, and whole
+// precision down to 2^-24 of the largest weight.
+constexpr float SHIFT = 10.f, SLACK = 5.f;
+
+struct TreeArgs {
+  egt_tree_batch b;
+  egt_kv_cache c;
+  float *part;                       // [splits][tokens * heads][dim]: weighted sums of a span
+  float2 *ml;                        // [splits][tokens * heads]: its reference and sum
+  int32_t shift, group, splits, row_blocks, min_tiles;
+  float scale2;                      // |scale| log2(e)
+  uint32_t flip;                     // sign of the scale, on pairs of q
+};
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s4v lds_s4v;
+
+__device__ __forceinline__ uint64_t lane_perm64(int lane, uint64_t v) {
+  const uint32_t lo = lane_perm(4 * lane, (uint32_t)v), hi = lane_perm(4 * lane, (uint32_t)(v >> 32));
+  return (uint64_t)hi << 32 | lo;
+}
+// 1 in the halves of a pair that are infinite or NaN, as whole-half masks
+__device__ __forceinline__ uint32_t odd_halves(uint32_t x) {
+  const uint32_t lo = (x & 0x7c00u) == 0x7c00u ? 0xffffu : 0u, hi = (x & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u;
+  return lo | hi;
+}
+
+// Units of 32 bytes of a key trade places by the key's number, so that the 16 keys of an operand read lie on different banks.
+// (Rows of an odd number of 64 bytes do so by themselves.)
+template <int DC>
+constexpr int SWIZZLE = DC == 4 || DC == 8 ? 7 : DC == 2 || DC == 6 ? 3 : 0;
+
+// How a request's keys are cut: the same answer in both kernels.
+struct Spans { int ctx_tiles, tiles, per, count; };
+__device__ __forceinline__ Spans spans_of(int len, int n, int splits, int min_tiles) {
+  Spans s;
+  s.ctx_tiles = (len + TILE - 1) / TILE;
+  s.tiles = s.ctx_tiles + (n + TILE - 1) / TILE;
+  s.per = max((s.tiles + splits - 1) / splits, min_tiles);
+  s.count = (s.tiles + s.per - 1) / s.per;
+  return s;
+}
+enum { ROWS_NONE, ROWS_BAD, ROWS_FINE };
+__device__ __forceinline__ int request_state(const TreeArgs &a, int t0, int t1, int len) {
+  if (t0 < 0 || t1 <= t0 || t1 > a.b.tokens) return ROWS_NONE;
+  return t1 - t0 > a.b.max_tokens || len < 0 || len > (int64_t)a.b.table_blocks << a.shift ? ROWS_BAD : ROWS_FINE;
+}
+
+template <int DC, int NR, int WR>
+__global__ __launch_bounds__(256, NR * DC <= 8 ? 2 : 1) void k_tree(TreeArgs a) {
+  // a key in LDS: ROW bytes, PIECES pieces of 16, a tile of K and one of V; a wave stages LJ x 64 pieces of either
+  constexpr int WK = 4 / WR, ROW = 64 * DC, PIECES = 4 * DC, LJ = (2 * DC + WR - 1) / WR, BUFS = WR > 1 ? 2 : 1, KV = TILE * ROW;
+  extern __shared__ __align__(16) uint8_t lds[];
+  __shared__ int odd_seen[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g4 = lane >> 4;
+  const int wr = wave % WR, wk = wave / WR, dim = a.c.dim;
+  const int r = blockIdx.z, kh = blockIdx.y / a.row_blocks, rb = blockIdx.y % a.row_blocks;
+  const int t0 = a.b.cu_tokens[r], t1 = a.b.cu_tokens[r + 1], len = a.b.lens[r];
+  const int state = request_state(a, t0, t1, len);
+  if (state == ROWS_NONE) return;
+  const int n = t1 - t0, rows = n * a.group;
+  if (state == ROWS_BAD) {
+    if (blockIdx.x == 0 && rb == 0)
+      for (int64_t e = threadIdx.x; e < (int64_t)rows * dim; e += 256) {
+        const int row = (int)(e / dim), d = (int)(e % dim);
+        a.b.out[(int64_t)(t0 + row / a.group) * a.b.out_row + (int64_t)(kh * a.group + row % a.group) * a.b.out_head + d] = 0x7e00;
+      }
     return;
   }
-  if (tid < c.dim) q[tid] = (float)((const __half *)b.q)[i * b.q_row + h * b.q_head + tid] * b.scale;
-  __syncthreads();
-  const uint64_t mask = b.mask[i];
-  float m = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = 64 * wave; k0 < len + n; k0 += 256) {
-    const int j = k0 + lane;
-    bool seen = false;
-    const __half *kp = nullptr;
-    if (j < len) {
-      const int block = b.block_table[(int64_t)r * b.ld_table + (j >> shift)];
-      seen = block >= 0 && block < c.blocks;
-      bad |= !seen;
-      kp = (const __half *)c.k + block * c.k_block + kh * c.k_head + (j & ((1 << shift) - 1)) * c.k_token;
-    } else if (j < len + n) {
-      seen = mask >> (j - len) & 1;
-      kp = (const __half *)b.k + (int64_t)(t0 + j - len) * b.k_row + kh * b.k_head;
+  const Spans sp = spans_of(len, n, a.splits, a.min_tiles);
+  const int row0 = rb * (16 * NR * WR);
+  if ((int)blockIdx.x >= sp.count || row0 >= rows) return;
+  const int base = row0 + wr * 16 * NR, begin = blockIdx.x * sp.per, end = min(begin + sp.per, sp.tiles);
+  if (threadIdx.x < 4) odd_seen[threadIdx.x] = 0;
+
+  // what a lane stages of a tile: piece `pc` of key `key` of K and of V, LJ times
+  const uint64_t safe = (uint64_t)(a.b.q + (int64_t)t0 * a.b.q_row);     // (dim readable values, for keys that are none)
+  const int32_t *table = a.b.block_table + (int64_t)r * a.b.ld_table;
+  uint8_t *group = lds + wk * (BUFS * 2 * KV);
+  bool bad = false;
+  auto key_of = [&](int x) { return (64 * (x * WR + wr) + lane) / PIECES; };
+  auto piece_of = [&](int x) { return (64 * (x * WR + wr) + lane) % PIECES; };
+  auto turn = [](int key) { return SWIZZLE<DC> == 7 ? key & 7 : SWIZZLE<DC> == 3 ? (key >> 1) & 3 : 0; };
+
+  auto page_of = [&](int t) -> int {
+    const int j = t * TILE + (lane & 31);
+    return t < sp.ctx_tiles && t < end && j < len ? table[j >> a.shift] : -1;
+  };
+  u4 kr[LJ], vr[LJ];
+  auto request = [&](int t, int page) {
+    const int j = t * TILE + (lane & 31);
+    uint64_t ka = safe, va = safe;
+    if (t < sp.ctx_tiles) {
+      if (j < len) {
+        if ((uint32_t)page < (uint32_t)a.c.blocks) {
+          const int64_t place = j & ((1 << a.shift) - 1);
+          ka = (uint64_t)(a.c.k + page * a.c.k_block + place * a.c.k_token + kh * a.c.k_head);
+          va = (uint64_t)(a.c.v + page * a.c.v_block + place * a.c.v_token + kh * a.c.v_head);
+        } else {
+          bad = true;
+        }
+      }
+    } else {
+      const int i = j - sp.ctx_tiles * TILE;
+      if (i < n) {
+        ka = (uint64_t)(a.b.k + (int64_t)(t0 + i) * a.b.k_row + kh * a.b.k_head);
+        va = (uint64_t)(a.b.v + (int64_t)(t0 + i) * a.b.v_row + kh * a.b.v_head);
+      }
     }
-    float s = -INFINITY;
-    if (seen) {
-      s = 0.f;
-      for (int d = 0; d < c.dim; ++d) s = fmaf(q[d], (float)kp[d], s);
+#pragma unroll
+    for (int x = 0; x < LJ; ++x) {
+      if (2 * DC % WR && x * WR + wr >= 2 * DC) break;
+      const int key = key_of(x), pc = piece_of(x), at = 16 * (8 * pc < dim ? pc : 0);
+      kr[x] = *(const u4 *)(lane_perm64(key, ka) + at);
+      vr[x] = *(const u4 *)(lane_perm64(key, va) + at);
     }
-    // (a NaN score has to stay one: fmaxf would drop it)
-    float top = s;
-    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
-    const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.f : mn, f = m == -INFINITY ? 0.f : expf(m - ref);
-    const float p = seen ? expf(s - ref) : 0.f;
-    float sum = p;
-    for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x, 64);
-    l = l * f + sum;
-    m = mn;
-    w[wave][lane] = p;
-    const uint64_t on = __ballot(seen);
-    for (int x = 0; x < 4; ++x) acc[x] *= f;
-    for (int x = 0; x < 64; ++x) {
-      if (!(on >> x & 1)) continue;
-      const int y = k0 + x;
-      const __half *vp;
-      if (y < len)
-        vp = (const __half *)c.v + b.block_table[(int64_t)r * b.ld_table + (y >> shift)] * c.v_block + kh * c.v_head + (y & ((1 << shift) - 1)) * c.v_token;
-      else
-        vp = (const __half *)b.v + (int64_t)(t0 + y - len) * b.v_row + kh * b.v_head;
-      for (int e = 0; e < 4; ++e)
-        if (lane + 64 * e < c.dim) acc[e] = fmaf(w[wave][x], (float)vp[lane + 64 * e], acc[e]);
+  };
+  auto stage = [&](int t, uint8_t *to) {
+    const bool drafted = t >= sp.ctx_tiles;
+    const int limit = drafted ? n - (t - sp.ctx_tiles) * TILE : len - t * TILE;
+    // columns past dim are zeros in K; values of keys that there are not become zeros, and so, for now, does what is not
+    // finite in drafted tokens: rows that do not see it must not meet it (0 times infinity)
+    if (dim != 32 * DC)
+#pragma unroll
+      for (int x = 0; x < LJ; ++x)
+        if (8 * piece_of(x) >= dim) kr[x] = u4{0, 0, 0, 0};
+    if (drafted || limit < TILE) {
+      bool odd = false;
+#pragma unroll
+      for (int x = 0; x < LJ; ++x) {
+        if (key_of(x) >= limit) vr[x] = u4{0, 0, 0, 0};
+        if (drafted) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t m = odd_halves(vr[x][e]);
+            odd |= m != 0;
+            vr[x][e] &= ~m;
+          }
+        }
+      }
+      if (odd) odd_seen[wk] = 1;
+    }
+#pragma unroll
+    for (int x = 0; x < LJ; ++x) {
+      if (2 * DC % WR && x * WR + wr >= 2 * DC) break;
+      const int key = key_of(x), pc = piece_of(x);
+      uint8_t *at = to + key * ROW + 32 * ((pc >> 1) ^ turn(key)) + 16 * (pc & 1);
+      *(u4 *)at = kr[x];
+      *(u4 *)(at + KV) = vr[x];
+    }
+  };
+
+  int t = begin + wk, page1 = -1;
+  if (t < end) {
+    const int page = page_of(t);
+    page1 = page_of(t + WK);
+    request(t, page);
+  }
+
+  // Q^T as the B operand: lane (g, n) holds d = 32 c + 8 g .. + 7 of row n
+  h8 q[NR][DC];
+#pragma unroll
+  for (int x = 0; x < NR; ++x) {
+    const int row = base + 16 * x + n16, tok = row / a.group;
+    const uint16_t *qp = a.b.q + (int64_t)(t0 + tok) * a.b.q_row + (int64_t)(kh * a.group + row - tok * a.group) * a.b.q_head;
+#pragma unroll
+    for (int c = 0; c < DC; ++c) {
+      u4 v = {0, 0, 0, 0};
+      if (row < rows && 32 * c + 8 * g4 < dim) {
+        v = *(const u4 *)(qp + 32 * c + 8 * g4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] ^= a.flip;
+      }
+      q[x][c] = __builtin_bit_cast(h8, v);
     }
   }
-  if (lane == 0) { ml[wave][0] = m; ml[wave][1] = l; }
-  for (int e = 0; e < 4; ++e) o[wave][lane + 64 * e] = acc[e];
+  f4 o[NR][2 * DC];
+  float ref[NR], off[NR], l[NR];                      // reference (base 2), SHIFT - reference, this lane's part of the sum
+#pragma unroll
+  for (int x = 0; x < NR; ++x) {
+    ref[x] = -INFINITY;
+    off[x] = SHIFT;
+    l[x] = 0.f;
+#pragma unroll
+    for (int d = 0; d < 2 * DC; ++d) o[x][d] = f4{0, 0, 0, 0};
+  }
+  __syncthreads();                                    // (odd_seen)
+
+  const int steps = (end - begin + WK - 1) / WK;      // (the same for every wave: they meet in a barrier)
+  for (int step = 0; step < steps; ++step, t += WK) {
+    uint8_t *tile = group + (BUFS > 1 ? (step & 1) * 2 * KV : 0);
+    if (t < end) {
+      stage(t, tile);
+      if (t + WK < end) {
+        request(t + WK, page1);
+        page1 = page_of(t + 2 * WK);
+      }
+    }
+    if (WR > 1) lds_barrier();                        // (two buffers: who writes the other one has passed this barrier, and so has every reader)
+    if (t >= end || base >= rows) continue;
+    const bool drafted = t >= sp.ctx_tiles;
+    const int limit = drafted ? n - (t - sp.ctx_tiles) * TILE : len - t * TILE;     // keys of the tile that there are
+    f4 s[NR][2];
+#pragma unroll
+    for (int x = 0; x < NR; ++x) s[x][0] = s[x][1] = f4{0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < DC; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int key = 16 * h + n16;
+        const h8 k = __builtin_bit_cast(h8, *(const u4 *)(tile + key * ROW + 32 * ((2 * c + (g4 >> 1)) ^ turn(key)) + 16 * (g4 & 1)));
+#pragma unroll
+        for (int x = 0; x < NR; ++x) s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[x][c], s[x][h], 0, 0, 0);
+      }
+    h8 p[NR];
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+      if (drafted || limit < TILE) {
+        const int row = base + 16 * x + n16;
+        const uint32_t word = !drafted ? ~0u : row < rows ? (uint32_t)(a.b.mask[t0 + row / a.group] >> ((t - sp.ctx_tiles) * TILE)) : 0u;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = 16 * h + 4 * g4 + i;
+            if (key >= limit || !(word >> key & 1)) s[x][h][i] = -INFINITY;
+          }
+      }
+      float top = fmaxf(fmaxf(fmaxf(s[x][0][0], s[x][0][1]), fmaxf(s[x][0][2], s[x][0][3])), fmaxf(fmaxf(s[x][1][0], s[x][1][1]), fmaxf(s[x][1][2], s[x][1][3])));
+      if (__any(top * a.scale2 > ref[x] + SLACK)) {
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64)) * a.scale2;
+        const float to = top > ref[x] + SLACK ? top : ref[x];
+        const float f = ref[x] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[x] - to);     // (nothing is there yet)
+        ref[x] = to;
+        off[x] = to == -INFINITY ? SHIFT : SHIFT - to;
+        l[x] *= f;
+#pragma unroll
+        for (int d = 0; d < 2 * DC; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[x][d][i] *= f;
+      }
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        e[i] = __builtin_amdgcn_exp2f(fmaf(s[x][i >> 2][i & 3], a.scale2, off[x]));
+        p[x][i] = (_Float16)e[i];
+      }
+      l[x] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+    }
+    // lane j of a group of 16 addresses 8 bytes of key 4 g + j / 4, and gets d = 16 dt + n of keys 4 g .. 4 g + 3
+#pragma unroll
+    for (int d = 0; d < 2 * DC; ++d) {
+      u4 v;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int key = 16 * h + 4 * g4 + (n16 >> 2);
+        const s4v w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(tile + KV + key * ROW + 32 * (d ^ turn(key)) + 8 * (n16 & 3)));
+        const u2 both = __builtin_bit_cast(u2, w);
+        v[2 * h] = both.x;
+        v[2 * h + 1] = both.y;
+      }
+#pragma unroll
+      for (int x = 0; x < NR; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, v), p[x], o[x][d], 0, 0, 0);
+    }
+    if (drafted && odd_seen[wk]) {                    // (rare) what was left out, to the rows that see it
+      for (int key = 0; key < min(limit, TILE); ++key) {
+        const uint16_t *vp = a.b.v + (int64_t)(t0 + (t - sp.ctx_tiles) * TILE + key) * a.b.v_row + kh * a.b.v_head;
+#pragma unroll
+        for (int x = 0; x < NR; ++x) {
+          const int row = base + 16 * x + n16;
+          if (row >= rows || !(a.b.mask[t0 + row / a.group] >> ((t - sp.ctx_tiles) * TILE + key) & 1)) continue;
+#pragma unroll
+          for (int d = 0; d < 2 * DC; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int at = 16 * d + 4 * g4 + i;
+              const uint16_t raw = at < dim ? vp[at] : 0;
+              if ((raw & 0x7c00) == 0x7c00) o[x][d][i] += (float)__builtin_bit_cast(_Float16, raw);
+            }
+        }
+      }
+    }
+  }
+
+  // the waves over the keys join: references and sums, then the weighted sums a row tile at a time through the V areas
+  __shared__ float refs[4][16 * NR], sums[4][16 * NR];
+#pragma unroll
+  for (int x = 0; x < NR; ++x) {
+    l[x] += __shfl_xor(l[x], 16, 64);
+    l[x] += __shfl_xor(l[x], 32, 64);
+    if (g4 == 0) {
+      refs[wave][16 * x + n16] = ref[x];
+      sums[wave][16 * x + n16] = l[x];
+    }
+  }
   bad = __syncthreads_or(bad);
-  float top = -INFINITY, total = 0.f, v = 0.f;
-  for (int x = 0; x < 4; ++x) top = fmaxf(top, ml[x][0]);
-  for (int x = 0; x < 4; ++x) {
-    const float f = ml[x][0] == -INFINITY ? (ml[x][1] == 0.f ? 0.f : 1.f) : expf(ml[x][0] - top);
-    total += f * ml[x][1];
-    v += f * o[x][tid & 255];
+#pragma unroll
+  for (int x = 0; x < NR; ++x) {
+    float top = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int w = 0; w < WK; ++w) top = fmaxf(top, refs[WR * w + wr][16 * x + n16]);
+    const float safe_top = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int w = 0; w < WK; ++w) {
+      const float rw = refs[WR * w + wr][16 * x + n16];
+      // (a wave without a reference has no weight, or only NaN: it keeps what it has)
+      total += (rw == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(rw - safe_top)) * sums[WR * w + wr][16 * x + n16];
+    }
+    const float f = ref[x] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[x] - safe_top);
+    if (WK > 1) {
+      float *area = (float *)(lds + wave * KV);
+      // row n of 16, d back to back; rows are shifted by their number so that a store of 16 rows spreads over the banks
+#pragma unroll
+      for (int d = 0; d < 2 * DC; ++d) {
+        f4 v = o[x][d];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] *= f;
+        *(f4 *)(area + n16 * (32 * DC) + 4 * ((4 * d + g4) ^ (n16 & 7))) = v;
+      }
+      __syncthreads();
+      // wave w of the WK takes a WK-th of the d tiles
+#pragma unroll
+      for (int d = 0; d < 2 * DC; ++d) {
+        if (d % WK != wk) continue;
+        f4 v = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < WK; ++w) {
+          const float *from = (const float *)(lds + (WR * w + wr) * KV);
+          const f4 u = *(const f4 *)(from + n16 * (32 * DC) + 4 * ((4 * d + g4) ^ (n16 & 7)));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] += u[i];
+        }
+        o[x][d] = v;
+      }
+    }
+    const int row = base + 16 * x + n16, tok = row / a.group, h = kh * a.group + row - tok * a.group;
+    if (row < rows) {
+      if (sp.count == 1) {
+        uint16_t *out = a.b.out + (int64_t)(t0 + tok) * a.b.out_row + (int64_t)h * a.b.out_head;
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+        for (int d = 0; d < 2 * DC; ++d) {
+          if (WK > 1 && d % WK != wk) continue;
+          const int at = 16 * d + 4 * g4;
+          if (at < dim) {
+            u2 w;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const h2 y = {(_Float16)(o[x][d][2 * i] * inv), (_Float16)(o[x][d][2 * i + 1] * inv)};
+              w[i] = bad ? 0x7e007e00u : __builtin_bit_cast(uint32_t, y);
+            }
+            *(u2 *)(out + at) = w;
+          }
+        }
+      } else {
+        const int64_t to = ((int64_t)blockIdx.x * a.b.tokens + t0 + tok) * a.b.heads + h;
+        if (wk == 0 && g4 == 0) a.ml[to] = float2{top, bad ? __builtin_nanf("") : total};
+#pragma unroll
+        for (int d = 0; d < 2 * DC; ++d) {
+          if (WK > 1 && d % WK != wk) continue;
+          const int at = 16 * d + 4 * g4;
+          if (at < dim) *(f4 *)(a.part + to * dim + at) = o[x][d];
+        }
+      }
+    }
+    if (WK > 1) __syncthreads();
   }
-  if (tid < c.dim) out[tid] = __float2half(bad ? __builtin_nanf("") : total == 0.f ? 0.f : v / total);
+}
+
+// The spans of a row join: one wave a row, in the order of the spans.
+__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
+  const int r = blockIdx.z, lane = threadIdx.x & 63, h = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int t0 = a.b.cu_tokens[r], t1 = a.b.cu_tokens[r + 1], len = a.b.lens[r], i = t0 + blockIdx.y;
+  if (request_state(a, t0, t1, len) != ROWS_FINE || i >= t1 || h >= a.b.heads) return;
+  const Spans sp = spans_of(len, t1 - t0, a.splits, a.min_tiles);
+  if (sp.count == 1) return;
+  const int64_t row = (int64_t)i * a.b.heads + h, step = (int64_t)a.b.tokens * a.b.heads;
+  float2 mine = lane < sp.count ? a.ml[lane * step + row] : float2{-INFINITY, 0.f};     // (64 spans at most)
+  float top = mine.x;
+#pragma unroll
+  for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+  const float w = mine.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mine.x - (top == -INFINITY ? 0.f : top));
+  float total = w * mine.y;
+#pragma unroll
+  for (int x = 32; x > 0; x >>= 1) total += __shfl_xor(total, x, 64);
+  f4 v = {0, 0, 0, 0};
+  const float *p = a.part + row * a.c.dim + (4 * lane < a.c.dim ? 4 * lane : 0);
+  for (int s = 0; s < sp.count; ++s) {
+    const float f = __shfl(w, s, 64);                 // (every lane is here: lane s may have no part of the row)
+    const f4 u = *(const f4 *)(p + s * step * a.c.dim);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fmaf(f, u[e], v[e]);
+  }
+  if (4 * lane < a.c.dim) {
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const h2 lo = {(_Float16)(v[0] * inv), (_Float16)(v[1] * inv)}, hi = {(_Float16)(v[2] * inv), (_Float16)(v[3] * inv)};
+    *(u2 *)(a.b.out + i * a.b.out_row + h * a.b.out_head + 4 * lane) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+  }
 }
 
 egt_status check_sizes(const egt_tree_batch *b, const egt_kv_cache *c) {
@@ -86,9 +431,49 @@ egt_status check_sizes(const egt_tree_batch *b, const egt_kv_cache *c) {
   if (b->requests < 0 || b->tokens < 0 || b->heads < 1 || b->heads % c->heads != 0 || b->max_tokens < 1 || b->max_tokens > EGT_MAX_TREE || b->table_blocks < 0 ||
       (int64_t)b->table_blocks * c->page >= (1ll << 31))
     return EGT_ERR_SHAPE;
-  return b->requests > EGT_MAX_REQUESTS || b->heads > 65535 ? EGT_ERR_UNSUPPORTED : EGT_OK;
+  return b->requests > EGT_MAX_REQUESTS || b->heads > 4096 ? EGT_ERR_UNSUPPORTED : EGT_OK;
 }
-size_t workspace_of(const egt_tree_batch *, const egt_kv_cache *) { return 16; }
+
+constexpr int MAX_SPLITS = 64;
+struct Shape { int nr, wr, row_blocks, splits, min_tiles; };
+Shape shape_of(const egt_tree_batch &b, const egt_kv_cache &c) {
+  Shape s;
+  const int rows = b.max_tokens * (b.heads / c.heads), most = c.dim <= 128 ? 4 : 2;
+  s.nr = rows <= 16 ? 1 : rows <= 32 ? 2 : most;
+  s.wr = rows <= 16 * s.nr ? 1 : rows <= 32 * s.nr ? 2 : 4;
+  s.row_blocks = (rows + 16 * s.nr * s.wr - 1) / (16 * s.nr * s.wr);
+  s.min_tiles = 4 / s.wr;
+  const int64_t groups = (int64_t)std::max(b.requests, 1) * c.heads * s.row_blocks, tiles = ((int64_t)b.table_blocks * c.page + TILE - 1) / TILE + 2;
+  s.splits = (int)std::min<int64_t>({std::max<int64_t>(512 / groups, 1), (tiles + s.min_tiles - 1) / s.min_tiles, MAX_SPLITS});
+  return s;
+}
+size_t rows_of(const egt_tree_batch &b) { return (size_t)b.tokens * b.heads; }
+size_t workspace_of(const egt_tree_batch &b, const egt_kv_cache &c) {
+  const Shape s = shape_of(b, c);
+  if (s.splits == 1) return 16;
+  return ((rows_of(b) * s.splits * 4 * (c.dim + 2) + 15) & ~(size_t)15) + 16;
+}
+
+template <int DC, int NR, int WR>
+hipError_t launch_tree(const TreeArgs &a, hipStream_t stream) {
+  constexpr size_t bytes = (size_t)(4 / WR) * (WR > 1 ? 2 : 1) * 2 * TILE * 64 * DC;
+  if (bytes > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute((const void *)k_tree<DC, NR, WR>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != hipSuccess) return e;
+  }
+  return launch(k_tree<DC, NR, WR>, dim3(a.splits, a.c.heads * a.row_blocks, a.b.requests), dim3(256), bytes, stream, a);
+}
+template <int DC>
+hipError_t launch_dim(const TreeArgs &a, const Shape &s, hipStream_t stream) {
+  constexpr int MOST = DC <= 4 ? 4 : 2;
+  if (s.nr == 1) return launch_tree<DC, 1, 1>(a, stream);
+  if (s.nr == 2 && s.wr == 1) return launch_tree<DC, 2, 1>(a, stream);
+  switch (s.wr) {
+    case 1: return launch_tree<DC, MOST, 1>(a, stream);
+    case 2: return launch_tree<DC, MOST, 2>(a, stream);
+    default: return launch_tree<DC, MOST, 4>(a, stream);
+  }
+}
 
 }  // namespace
 }  // namespace egt
@@ -98,7 +483,7 @@ extern "C" {
 egt_status egt_tree_attention_ws_bytes(const egt_tree_batch *b, const egt_kv_cache *cache, size_t *bytes) {
   if (!bytes) return EGT_ERR_NULL;
   const egt_status st = egt::check_sizes(b, cache);
-  if (st == EGT_OK) *bytes = egt::workspace_of(b, cache);
+  if (st == EGT_OK) *bytes = egt::workspace_of(*b, *cache);
   return st;
 }
 
@@ -110,13 +495,35 @@ egt_status egt_tree_attention(const egt_tree_batch *b, const egt_kv_cache *cache
   if (b->ld_table < b->table_blocks || !(b->scale == b->scale)) return EGT_ERR_SHAPE;
   if (b->requests == 0 || b->tokens == 0) return EGT_OK;
   if (!b->q || !b->k || !b->v || !b->out || !b->lens || !b->cu_tokens || !b->mask || (b->table_blocks && !b->block_table) || !workspace) return EGT_ERR_NULL;
-  if (workspace_bytes < egt::workspace_of(b, cache)) return EGT_ERR_SHAPE;
+  if (workspace_bytes < egt::workspace_of(*b, *cache)) return EGT_ERR_SHAPE;
   if (!egt::whole16(b->q) || !egt::whole16(b->k) || !egt::whole16(b->v) || !egt::whole16(b->out) || !egt::whole16(workspace) ||
       !egt::whole8(b->q_row, b->q_head, b->k_row, b->k_head, b->v_row, b->v_head, b->out_row, b->out_head) || ((uintptr_t)b->mask & 7) ||
       ((uintptr_t)b->lens & 3) || ((uintptr_t)b->cu_tokens & 3) || ((uintptr_t)b->block_table & 3))
     return EGT_ERR_BUFFER;
-  return egt::answer(egt::launch(egt::k_tree_simple, dim3(b->max_tokens, b->heads, b->requests), dim3(256), 0, (hipStream_t)stream, *b, *cache,
-                                 egt::log2_of(cache->page)));
+  const egt::Shape s = egt::shape_of(*b, *cache);
+  egt::TreeArgs a;
+  a.b = *b;
+  a.c = *cache;
+  a.part = (float *)workspace;
+  a.ml = (float2 *)(a.part + (egt::rows_of(*b) * s.splits * cache->dim + 3) / 4 * 4);
+  a.shift = egt::log2_of(cache->page);
+  a.group = b->heads / cache->heads;
+  a.splits = s.splits;
+  a.row_blocks = s.row_blocks;
+  a.min_tiles = s.min_tiles;
+  a.scale2 = __builtin_fabsf(b->scale) * 1.44269504088896340736f;
+  a.flip = __builtin_signbit(b->scale) ? 0x80008000u : 0u;
+  const hipStream_t to = (hipStream_t)stream;
+  hipError_t e;
+  switch ((cache->dim + 31) / 32) {
+    case 1: case 2: e = egt::launch_dim<2>(a, s, to); break;
+    case 3: e = egt::launch_dim<3>(a, s, to); break;
+    case 4: e = egt::launch_dim<4>(a, s, to); break;
+    case 5: case 6: e = egt::launch_dim<6>(a, s, to); break;
+    default: e = egt::launch_dim<8>(a, s, to); break;
+  }
+  if (e == hipSuccess && s.splits > 1) e = egt::launch(egt::k_tree_join, dim3((b->heads + 3) / 4, b->max_tokens, b->requests), dim3(256), 0, to, a);
+  return egt::answer(e);
 }
 
 }  // extern "C"
