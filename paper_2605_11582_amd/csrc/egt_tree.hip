@@ -36,14 +36,10 @@ struct TreeArgs {
   uint32_t flip;                     // sign of the scale, on pairs of q
 };
 
-typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) u4 global_u4;
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s4v lds_s4v;
 
-__device__ __forceinline__ uint64_t lane_perm64(int lane, uint64_t v) {
-  const uint32_t lo = lane_perm(4 * lane, (uint32_t)v), hi = lane_perm(4 * lane, (uint32_t)(v >> 32));
-  return (uint64_t)hi << 32 | lo;
-}
 // 1 in the halves of a pair that are infinite or NaN, as whole-half masks
 __device__ __forceinline__ uint32_t odd_halves(uint32_t x) {
   const uint32_t lo = (x & 0x7c00u) == 0x7c00u ? 0xffffu : 0u, hi = (x & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u;
@@ -68,15 +64,20 @@ __device__ __forceinline__ Spans spans_of(int len, int n, int splits, int min_ti
 enum { ROWS_NONE, ROWS_BAD, ROWS_FINE };
 __device__ __forceinline__ int request_state(const TreeArgs &a, int t0, int t1, int len) {
   if (t0 < 0 || t1 <= t0 || t1 > a.b.tokens) return ROWS_NONE;
-  return t1 - t0 > a.b.max_tokens || len < 0 || len > (int64_t)a.b.table_blocks << a.shift ? ROWS_BAD : ROWS_FINE;
+  return t1 - t0 > a.b.max_tokens || len < 0 || len > (int64_t)a.b.table_blocks << a.shift || (len > 0 && a.c.blocks == 0) ? ROWS_BAD : ROWS_FINE;
 }
 
+// Waves of a workgroup, and how many tiles ahead of their use a wave requests its share of them.
+constexpr int waves_of(int wr) { return wr > 4 ? wr : 4; }
+constexpr int ahead_of(int wr) { return wr >= 8 ? 3 : wr >= 2 ? 2 : 1; }
+
 template <int DC, int NR, int WR>
-__global__ __launch_bounds__(256, NR * DC <= 8 ? 2 : 1) void k_tree(TreeArgs a) {
+__global__ __launch_bounds__(64 * waves_of(WR), 2) void k_tree(TreeArgs a) {
   // a key in LDS: ROW bytes, PIECES pieces of 16, a tile of K and one of V; a wave stages LJ x 64 pieces of either
-  constexpr int WK = 4 / WR, ROW = 64 * DC, PIECES = 4 * DC, LJ = (2 * DC + WR - 1) / WR, BUFS = WR > 1 ? 2 : 1, KV = TILE * ROW;
+  constexpr int W = waves_of(WR), WK = W / WR, ROW = 64 * DC, PIECES = 4 * DC, LJ = (2 * DC + WR - 1) / WR, BUFS = WR > 1 ? 2 : 1, KV = TILE * ROW;
+  constexpr int AHEAD = ahead_of(WR);
   extern __shared__ __align__(16) uint8_t lds[];
-  __shared__ int odd_seen[4];
+  __shared__ int odd_seen[W];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g4 = lane >> 4;
   const int wr = wave % WR, wk = wave / WR, dim = a.c.dim;
   const int r = blockIdx.z, kh = blockIdx.y / a.row_blocks, rb = blockIdx.y % a.row_blocks;
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(256, NR * DC <= 8 ? 2 : 1) void k_tree(TreeArgs a) 
   const int n = t1 - t0, rows = n * a.group;
   if (state == ROWS_BAD) {
     if (blockIdx.x == 0 && rb == 0)
-      for (int64_t e = threadIdx.x; e < (int64_t)rows * dim; e += 256) {
+      for (int64_t e = threadIdx.x; e < (int64_t)rows * dim; e += 64 * W) {
         const int row = (int)(e / dim), d = (int)(e % dim);
         a.b.out[(int64_t)(t0 + row / a.group) * a.b.out_row + (int64_t)(kh * a.group + row % a.group) * a.b.out_head + d] = 0x7e00;
       }
@@ -96,51 +97,57 @@ __global__ __launch_bounds__(256, NR * DC <= 8 ? 2 : 1) void k_tree(TreeArgs a) 
   const int row0 = rb * (16 * NR * WR);
   if ((int)blockIdx.x >= sp.count || row0 >= rows) return;
   const int base = row0 + wr * 16 * NR, begin = blockIdx.x * sp.per, end = min(begin + sp.per, sp.tiles);
-  if (threadIdx.x < 4) odd_seen[threadIdx.x] = 0;
+  if (threadIdx.x < W) odd_seen[threadIdx.x] = 0;
 
   // what a lane stages of a tile: piece `pc` of key `key` of K and of V, LJ times
-  const uint64_t safe = (uint64_t)(a.b.q + (int64_t)t0 * a.b.q_row);     // (dim readable values, for keys that are none)
   const int32_t *table = a.b.block_table + (int64_t)r * a.b.ld_table;
+  const int pmask = (1 << a.shift) - 1;
   uint8_t *group = lds + wk * (BUFS * 2 * KV);
   bool bad = false;
+  auto there = [&](int x) { return 2 * DC % WR == 0 || x * WR + wr < 2 * DC; };
   auto key_of = [&](int x) { return (64 * (x * WR + wr) + lane) / PIECES; };
   auto piece_of = [&](int x) { return (64 * (x * WR + wr) + lane) % PIECES; };
   auto turn = [](int key) { return SWIZZLE<DC> == 7 ? key & 7 : SWIZZLE<DC> == 3 ? (key >> 1) & 3 : 0; };
 
-  auto page_of = [&](int t) -> int {
-    const int j = t * TILE + (lane & 31);
-    return t < sp.ctx_tiles && t < end && j < len ? table[j >> a.shift] : -1;
-  };
-  u4 kr[LJ], vr[LJ];
-  auto request = [&](int t, int page) {
-    const int j = t * TILE + (lane & 31);
-    uint64_t ka = safe, va = safe;
-    if (t < sp.ctx_tiles) {
-      if (j < len) {
-        if ((uint32_t)page < (uint32_t)a.c.blocks) {
-          const int64_t place = j & ((1 << a.shift) - 1);
-          ka = (uint64_t)(a.c.k + page * a.c.k_block + place * a.c.k_token + kh * a.c.k_head);
-          va = (uint64_t)(a.c.v + page * a.c.v_block + place * a.c.v_token + kh * a.c.v_head);
-        } else {
-          bad = true;
-        }
-      }
-    } else {
-      const int i = j - sp.ctx_tiles * TILE;
-      if (i < n) {
-        ka = (uint64_t)(a.b.k + (int64_t)(t0 + i) * a.b.k_row + kh * a.b.k_head);
-        va = (uint64_t)(a.b.v + (int64_t)(t0 + i) * a.b.v_row + kh * a.b.v_head);
-      }
-    }
+  // (a tile begins on a page or lies inside one: its keys' pages and places are its own first one's, plus theirs)
+  struct Pages { int at[LJ]; };
+  auto pages_of = [&](int t) {
+    Pages p;
 #pragma unroll
     for (int x = 0; x < LJ; ++x) {
-      if (2 * DC % WR && x * WR + wr >= 2 * DC) break;
-      const int key = key_of(x), pc = piece_of(x), at = 16 * (8 * pc < dim ? pc : 0);
-      kr[x] = *(const u4 *)(lane_perm64(key, ka) + at);
-      vr[x] = *(const u4 *)(lane_perm64(key, va) + at);
+      const int key = key_of(x);
+      p.at[x] = 0;
+      if (there(x) && t < end && t < sp.ctx_tiles && t * TILE + key < len) p.at[x] = table[((t * TILE) >> a.shift) + (key >> a.shift)];
     }
+    return p;
   };
-  auto stage = [&](int t, uint8_t *to) {
+  struct Staged { u4 k[LJ], v[LJ]; };
+  auto request = [&](int t, const Pages &page) {
+    Staged s;
+    const bool drafted = t >= sp.ctx_tiles;
+#pragma unroll
+    for (int x = 0; x < LJ; ++x) {
+      if (!there(x)) break;
+      const int key = key_of(x), pc = piece_of(x), d = 8 * pc < dim ? 8 * pc : 0;
+      uint64_t ka, va;
+      if (!drafted) {
+        // (a page that is not the cache's: NaN in the end, and page 0 meanwhile)
+        const bool fine = (uint32_t)page.at[x] < (uint32_t)a.c.blocks;
+        bad |= !fine;
+        const uint64_t block = fine ? page.at[x] : 0, place = ((t * TILE) & pmask) + (key & pmask);
+        ka = (uint64_t)(a.c.k + kh * a.c.k_head) + 2 * (block * a.c.k_block + place * a.c.k_token);
+        va = (uint64_t)(a.c.v + kh * a.c.v_head) + 2 * (block * a.c.v_block + place * a.c.v_token);
+      } else {
+        const uint64_t i = t0 + min((t - sp.ctx_tiles) * TILE + key, n - 1);
+        ka = (uint64_t)(a.b.k + kh * a.b.k_head) + 2 * i * a.b.k_row;
+        va = (uint64_t)(a.b.v + kh * a.b.v_head) + 2 * i * a.b.v_row;
+      }
+      s.k[x] = *(const global_u4 *)(ka + 2 * d);
+      s.v[x] = *(const global_u4 *)(va + 2 * d);
+    }
+    return s;
+  };
+  auto stage = [&](int t, Staged &s, uint8_t *to) {
     const bool drafted = t >= sp.ctx_tiles;
     const int limit = drafted ? n - (t - sp.ctx_tiles) * TILE : len - t * TILE;
     // columns past dim are zeros in K; values of keys that there are not become zeros, and so, for now, does what is not
@@ -148,18 +155,19 @@ __global__ __launch_bounds__(256, NR * DC <= 8 ? 2 : 1) void k_tree(TreeArgs a) 
     if (dim != 32 * DC)
 #pragma unroll
       for (int x = 0; x < LJ; ++x)
-        if (8 * piece_of(x) >= dim) kr[x] = u4{0, 0, 0, 0};
+        if (8 * piece_of(x) >= dim) s.k[x] = u4{0, 0, 0, 0};
     if (drafted || limit < TILE) {
       bool odd = false;
 #pragma unroll
       for (int x = 0; x < LJ; ++x) {
-        if (key_of(x) >= limit) vr[x] = u4{0, 0, 0, 0};
+        if (!there(x)) break;
+        if (key_of(x) >= limit) s.v[x] = u4{0, 0, 0, 0};
         if (drafted) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const uint32_t m = odd_halves(vr[x][e]);
+            const uint32_t m = odd_halves(s.v[x][e]);
             odd |= m != 0;
-            vr[x][e] &= ~m;
+            s.v[x][e] &= ~m;
           }
         }
       }
@@ -167,19 +175,26 @@ __global__ __launch_bounds__(256, NR * DC <= 8 ? 2 : 1) void k_tree(TreeArgs a) 
     }
 #pragma unroll
     for (int x = 0; x < LJ; ++x) {
-      if (2 * DC % WR && x * WR + wr >= 2 * DC) break;
+      if (!there(x)) break;
       const int key = key_of(x), pc = piece_of(x);
       uint8_t *at = to + key * ROW + 32 * ((pc >> 1) ^ turn(key)) + 16 * (pc & 1);
-      *(u4 *)at = kr[x];
-      *(u4 *)(at + KV) = vr[x];
+      *(u4 *)at = s.k[x];
+      *(u4 *)(at + KV) = s.v[x];
     }
   };
 
-  int t = begin + wk, page1 = -1;
-  if (t < end) {
-    const int page = page_of(t);
-    page1 = page_of(t + WK);
-    request(t, page);
+  // tiles t, t + WK, ... t + (AHEAD - 1) WK are on their way, the page numbers of the next one too
+  int t = begin + wk;
+  Staged ring[AHEAD];
+  Pages next;
+  {
+    Pages p[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) p[i] = pages_of(t + i * WK);
+    next = pages_of(t + AHEAD * WK);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (t + i * WK < end) ring[i] = request(t + i * WK, p[i]);
   }
 
   // Q^T as the B operand: lane (g, n) holds d = 32 c + 8 g .. + 7 of row n
@@ -215,11 +230,11 @@ __global__ __launch_bounds__(256, NR * DC <= 8 ? 2 : 1) void k_tree(TreeArgs a) 
   for (int step = 0; step < steps; ++step, t += WK) {
     uint8_t *tile = group + (BUFS > 1 ? (step & 1) * 2 * KV : 0);
     if (t < end) {
-      stage(t, tile);
-      if (t + WK < end) {
-        request(t + WK, page1);
-        page1 = page_of(t + 2 * WK);
-      }
+      stage(t, ring[0], tile);
+#pragma unroll
+      for (int i = 0; i + 1 < AHEAD; ++i) ring[i] = ring[i + 1];
+      if (t + AHEAD * WK < end) ring[AHEAD - 1] = request(t + AHEAD * WK, next);
+      next = pages_of(t + (AHEAD + 1) * WK);
     }
     if (WR > 1) lds_barrier();                        // (two buffers: who writes the other one has passed this barrier, and so has every reader)
     if (t >= end || base >= rows) continue;
@@ -288,28 +303,10 @@ __global__ __launch_bounds__(256, NR * DC <= 8 ? 2 : 1) void k_tree(TreeArgs a) 
 #pragma unroll
       for (int x = 0; x < NR; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, v), p[x], o[x][d], 0, 0, 0);
     }
-    if (drafted && odd_seen[wk]) {                    // (rare) what was left out, to the rows that see it
-      for (int key = 0; key < min(limit, TILE); ++key) {
-        const uint16_t *vp = a.b.v + (int64_t)(t0 + (t - sp.ctx_tiles) * TILE + key) * a.b.v_row + kh * a.b.v_head;
-#pragma unroll
-        for (int x = 0; x < NR; ++x) {
-          const int row = base + 16 * x + n16;
-          if (row >= rows || !(a.b.mask[t0 + row / a.group] >> ((t - sp.ctx_tiles) * TILE + key) & 1)) continue;
-#pragma unroll
-          for (int d = 0; d < 2 * DC; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int at = 16 * d + 4 * g4 + i;
-              const uint16_t raw = at < dim ? vp[at] : 0;
-              if ((raw & 0x7c00) == 0x7c00) o[x][d][i] += (float)__builtin_bit_cast(_Float16, raw);
-            }
-        }
-      }
-    }
   }
 
   // the waves over the keys join: references and sums, then the weighted sums a row tile at a time through the V areas
-  __shared__ float refs[4][16 * NR], sums[4][16 * NR];
+  __shared__ float refs[W][16 * NR], sums[W][16 * NR];
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
     l[x] += __shfl_xor(l[x], 16, 64);
@@ -320,6 +317,30 @@ __global__ __launch_bounds__(256, NR * DC <= 8 ? 2 : 1) void k_tree(TreeArgs a) 
     }
   }
   bad = __syncthreads_or(bad);
+  if (odd_seen[wk] && base < rows) {                  // (rare) what is not finite in drafted tokens, to the rows that see it
+    const int first = max(begin, sp.ctx_tiles);
+    for (int key = 0; key < min((end - sp.ctx_tiles) * TILE, n); ++key) {
+      const int of = sp.ctx_tiles + key / TILE;
+      if (of < first || (of - begin) % WK != wk) continue;
+      const uint16_t *vp = a.b.v + (int64_t)(t0 + key) * a.b.v_row + kh * a.b.v_head;
+#pragma unroll
+      for (int x = 0; x < NR; ++x) {
+        const int row = base + 16 * x + n16;
+        if (row >= rows || !(a.b.mask[t0 + row / a.group] >> key & 1)) continue;
+#pragma unroll
+        for (int d = 0; d < 2 * DC; ++d) {
+          const int at = 16 * d + 4 * g4;
+          if (at >= dim) continue;
+          const u2 four = *(const u2 *)(vp + at);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint16_t raw = (uint16_t)(four[i >> 1] >> 16 * (i & 1));
+            if ((raw & 0x7c00) == 0x7c00) o[x][d][i] += (float)__builtin_bit_cast(_Float16, raw);
+          }
+        }
+      }
+    }
+  }
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
     float top = -INFINITY, total = 0.f;
@@ -411,6 +432,7 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
   for (int x = 32; x > 0; x >>= 1) total += __shfl_xor(total, x, 64);
   f4 v = {0, 0, 0, 0};
   const float *p = a.part + row * a.c.dim + (4 * lane < a.c.dim ? 4 * lane : 0);
+#pragma unroll 8
   for (int s = 0; s < sp.count; ++s) {
     const float f = __shfl(w, s, 64);                 // (every lane is here: lane s may have no part of the row)
     const f4 u = *(const f4 *)(p + s * step * a.c.dim);
@@ -438,13 +460,14 @@ constexpr int MAX_SPLITS = 64;
 struct Shape { int nr, wr, row_blocks, splits, min_tiles; };
 Shape shape_of(const egt_tree_batch &b, const egt_kv_cache &c) {
   Shape s;
-  const int rows = b.max_tokens * (b.heads / c.heads), most = c.dim <= 128 ? 4 : 2;
-  s.nr = rows <= 16 ? 1 : rows <= 32 ? 2 : most;
-  s.wr = rows <= 16 * s.nr ? 1 : rows <= 32 * s.nr ? 2 : 4;
+  const int rows = b.max_tokens * (b.heads / c.heads);
+  s.nr = rows <= 16 || c.dim > 128 ? 1 : 2;
+  s.wr = 1;
+  while (s.wr < 8 && rows > 16 * s.nr * s.wr) s.wr *= 2;
   s.row_blocks = (rows + 16 * s.nr * s.wr - 1) / (16 * s.nr * s.wr);
-  s.min_tiles = 4 / s.wr;
+  s.min_tiles = waves_of(s.wr) / s.wr;
   const int64_t groups = (int64_t)std::max(b.requests, 1) * c.heads * s.row_blocks, tiles = ((int64_t)b.table_blocks * c.page + TILE - 1) / TILE + 2;
-  s.splits = (int)std::min<int64_t>({std::max<int64_t>(512 / groups, 1), (tiles + s.min_tiles - 1) / s.min_tiles, MAX_SPLITS});
+  s.splits = (int)std::min<int64_t>({std::max<int64_t>((s.wr == 8 ? 256 : 512) / groups, 1), (tiles + s.min_tiles - 1) / s.min_tiles, MAX_SPLITS});
   return s;
 }
 size_t rows_of(const egt_tree_batch &b) { return (size_t)b.tokens * b.heads; }
@@ -456,22 +479,22 @@ size_t workspace_of(const egt_tree_batch &b, const egt_kv_cache &c) {
 
 template <int DC, int NR, int WR>
 hipError_t launch_tree(const TreeArgs &a, hipStream_t stream) {
-  constexpr size_t bytes = (size_t)(4 / WR) * (WR > 1 ? 2 : 1) * 2 * TILE * 64 * DC;
-  if (bytes > 64 * 1024) {
+  constexpr size_t bytes = (size_t)(waves_of(WR) / WR) * (WR > 1 ? 2 : 1) * 2 * TILE * 64 * DC;
+  if (bytes > 60 * 1024) {
     const hipError_t e = hipFuncSetAttribute((const void *)k_tree<DC, NR, WR>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e != hipSuccess) return e;
   }
-  return launch(k_tree<DC, NR, WR>, dim3(a.splits, a.c.heads * a.row_blocks, a.b.requests), dim3(256), bytes, stream, a);
+  return launch(k_tree<DC, NR, WR>, dim3(a.splits, a.c.heads * a.row_blocks, a.b.requests), dim3(64 * waves_of(WR)), bytes, stream, a);
 }
 template <int DC>
 hipError_t launch_dim(const TreeArgs &a, const Shape &s, hipStream_t stream) {
-  constexpr int MOST = DC <= 4 ? 4 : 2;
-  if (s.nr == 1) return launch_tree<DC, 1, 1>(a, stream);
-  if (s.nr == 2 && s.wr == 1) return launch_tree<DC, 2, 1>(a, stream);
+  constexpr int NR = DC <= 4 ? 2 : 1;
+  if (s.nr == 1 && s.wr == 1) return launch_tree<DC, 1, 1>(a, stream);
   switch (s.wr) {
-    case 1: return launch_tree<DC, MOST, 1>(a, stream);
-    case 2: return launch_tree<DC, MOST, 2>(a, stream);
-    default: return launch_tree<DC, MOST, 4>(a, stream);
+    case 1: return launch_tree<DC, NR, 1>(a, stream);
+    case 2: return launch_tree<DC, NR, 2>(a, stream);
+    case 4: return launch_tree<DC, NR, 4>(a, stream);
+    default: return launch_tree<DC, NR, 8>(a, stream);
   }
 }
 
