@@ -492,9 +492,9 @@ egt_status egt_kv_append(const egt_append_batch *b, const egt_kv_cache *cache, v
  * caller's bound, requests with more get NaN.  NaN also where a length is negative or longer than
  * the table's row, or where a page in use is not one of the cache's.
  * FP16 in and out; scores, maxima, sums and the weighted sum in FP32, the weights rounded to
- * FP16 for the matrix cores (relative to the largest, down to 2^-28 of it).
- * dim: a multiple of 8 up to 256; pointers and strides whole 16 bytes; k and v are read in the
- * cache's head count.  `out` must not overlap an input.
+ * FP16 for the matrix cores (relative to the largest, down to 2^-24 of it).
+ * dim: a multiple of 8 up to 256; pointers and strides whole 16 bytes; k and v have the cache's heads;
+ * the pages of the cache, and the tokens of a page, lie less than 2^31 elements apart.  `out` must not overlap an input.
  * egt_tree_attention_ws_bytes (HOST): bytes of workspace (DEVICE, 16-byte aligned) that a call
  * of these requests, tokens, heads, max_tokens, table_blocks and cache sizes needs, never less
  * than 16; the pointers are not looked at.  The workspace is dead after the call's kernels; calls that share one must not overlap.

@@ -24,7 +24,7 @@ namespace {
 constexpr int TILE = 32;             // keys a wave takes at a time
 // p is held as 2^SHIFT p against its reference, and may pass it by 2^SLACK: 2^15 at most in FP16, and whole
 // precision down to 2^-24 of the largest weight.
-constexpr float SHIFT = 10.f, SLACK = 5.f;
+constexpr float SHIFT = 10.f, SLACK = 5.f, EXP2_LIMIT = 32768.f;
 
 struct TreeArgs {
   egt_tree_batch b;
@@ -69,11 +69,11 @@ __device__ __forceinline__ int request_state(const TreeArgs &a, int t0, int t1, 
 
 // Waves of a workgroup, and how many tiles ahead of their use a wave requests its share of them.
 constexpr int waves_of(int wr) { return wr > 4 ? wr : 4; }
-constexpr int ahead_of(int wr) { return wr >= 8 ? 3 : wr >= 2 ? 2 : 1; }
+constexpr int ahead_of(int wr) { return wr >= 8 ? 3 : wr >= 4 ? 2 : 1; }
 
 template <int DC, int NR, int WR>
-__global__ __launch_bounds__(64 * waves_of(WR), 2) void k_tree(TreeArgs a) {
-  // a key in LDS: ROW bytes, PIECES pieces of 16, a tile of K and one of V; a wave stages LJ x 64 pieces of either
+__global__ __launch_bounds__(64 * waves_of(WR), DC > 4 && WR < 8 ? 1 : 2) void k_tree(TreeArgs a) {
+  // a key in LDS: ROW bytes, PIECES pieces of 16; a tile of K and one of V: KV bytes each; a wave stages LJ x 64 pieces of either
   constexpr int W = waves_of(WR), WK = W / WR, ROW = 64 * DC, PIECES = 4 * DC, LJ = (2 * DC + WR - 1) / WR, BUFS = WR > 1 ? 2 : 1, KV = TILE * ROW;
   constexpr int AHEAD = ahead_of(WR);
   extern __shared__ __align__(16) uint8_t lds[];
@@ -97,105 +97,117 @@ __global__ __launch_bounds__(64 * waves_of(WR), 2) void k_tree(TreeArgs a) {
   const int row0 = rb * (16 * NR * WR);
   if ((int)blockIdx.x >= sp.count || row0 >= rows) return;
   const int base = row0 + wr * 16 * NR, begin = blockIdx.x * sp.per, end = min(begin + sp.per, sp.tiles);
-  if (threadIdx.x < W) odd_seen[threadIdx.x] = 0;
+  const bool busy = base < rows;                      // (a wave without rows still stages its share)
+  // This wave's tiles are begin + wk + i WK, i < mine; all waves go `steps` steps, for they meet in barriers.  Steps and requests
+  // past the last tile take that one again, with every key masked.
+  const int steps = (end - begin + WK - 1) / WK, mine = (end - begin - wk + WK - 1) / WK;
+  auto tile_of = [&](int i) { return min(begin + wk + i * WK, end - 1); };
+  auto limit_of = [&](int i) {                        // keys that there are
+    const int t = tile_of(i);
+    return i >= mine ? 0 : t >= sp.ctx_tiles ? n - (t - sp.ctx_tiles) * TILE : len - t * TILE;
+  };
 
-  // what a lane stages of a tile: piece `pc` of key `key` of K and of V, LJ times
-  const int32_t *table = a.b.block_table + (int64_t)r * a.b.ld_table;
-  const int pmask = (1 << a.shift) - 1;
-  uint8_t *group = lds + wk * (BUFS * 2 * KV);
-  bool bad = false;
   auto there = [&](int x) { return 2 * DC % WR == 0 || x * WR + wr < 2 * DC; };
   auto key_of = [&](int x) { return (64 * (x * WR + wr) + lane) / PIECES; };
   auto piece_of = [&](int x) { return (64 * (x * WR + wr) + lane) % PIECES; };
   auto turn = [](int key) { return SWIZZLE<DC> == 7 ? key & 7 : SWIZZLE<DC> == 3 ? (key >> 1) & 3 : 0; };
 
-  // (a tile begins on a page or lies inside one: its keys' pages and places are its own first one's, plus theirs)
+  // What a lane requests of a tile: piece `piece_of(x)` of key `key_of(x)`, LJ times.  Cached and drafted keys differ in numbers alone:
+  // a drafted one is place i of a page 0 that begins at the request's first row.
+  const int32_t *table = len > 0 ? a.b.block_table + (int64_t)r * a.b.ld_table : a.b.lens;
+  const int pmask = (1 << a.shift) - 1;
   struct Pages { int at[LJ]; };
-  auto pages_of = [&](int t) {
+  auto pages_of = [&](int i) {
+    const int t = tile_of(i);
     Pages p;
 #pragma unroll
-    for (int x = 0; x < LJ; ++x) {
-      const int key = key_of(x);
-      p.at[x] = 0;
-      if (there(x) && t < end && t < sp.ctx_tiles && t * TILE + key < len) p.at[x] = table[((t * TILE) >> a.shift) + (key >> a.shift)];
-    }
-    return p;
+    for (int x = 0; x < LJ; ++x) p.at[x] = table[max(min(t * TILE + key_of(x), len - 1), 0) >> a.shift];
+    return p;                                         // (not looked at here: a look would wait for it)
   };
-  struct Staged { u4 k[LJ], v[LJ]; };
-  auto request = [&](int t, const Pages &page) {
-    Staged s;
+  uint32_t worst = 0;                                 // the largest page number met
+  struct Share { u4 at[LJ]; };
+  auto request = [&](int i, const Pages &page, const uint16_t *cached, int64_t block_step, int64_t token_step, const uint16_t *drafts, int64_t row_step) {
+    const int t = tile_of(i);
     const bool drafted = t >= sp.ctx_tiles;
+    const uint16_t *from = drafted ? drafts : cached;
+    const uint32_t ts = 2 * (uint32_t)(drafted ? row_step : token_step), bs = 2 * (uint32_t)block_step;
+    const int first = (drafted ? t - sp.ctx_tiles : t) * TILE, within = drafted ? -1 : pmask, most = drafted ? n - 1 : INT32_MAX;
+    Share s;
 #pragma unroll
     for (int x = 0; x < LJ; ++x) {
       if (!there(x)) break;
-      const int key = key_of(x), pc = piece_of(x), d = 8 * pc < dim ? 8 * pc : 0;
-      uint64_t ka, va;
-      if (!drafted) {
-        // (a page that is not the cache's: NaN in the end, and page 0 meanwhile)
-        const bool fine = (uint32_t)page.at[x] < (uint32_t)a.c.blocks;
-        bad |= !fine;
-        const uint64_t block = fine ? page.at[x] : 0, place = ((t * TILE) & pmask) + (key & pmask);
-        ka = (uint64_t)(a.c.k + kh * a.c.k_head) + 2 * (block * a.c.k_block + place * a.c.k_token);
-        va = (uint64_t)(a.c.v + kh * a.c.v_head) + 2 * (block * a.c.v_block + place * a.c.v_token);
-      } else {
-        const uint64_t i = t0 + min((t - sp.ctx_tiles) * TILE + key, n - 1);
-        ka = (uint64_t)(a.b.k + kh * a.b.k_head) + 2 * i * a.b.k_row;
-        va = (uint64_t)(a.b.v + kh * a.b.v_head) + 2 * i * a.b.v_row;
-      }
-      s.k[x] = *(const global_u4 *)(ka + 2 * d);
-      s.v[x] = *(const global_u4 *)(va + 2 * d);
+      const uint32_t number = drafted ? 0u : (uint32_t)page.at[x];
+      worst = max(worst, number);                     // (one that is not the cache's: NaN in the end, and the last one meanwhile)
+      const uint32_t block = min(number, (uint32_t)max(a.c.blocks - 1, 0)), place = min((first + key_of(x)) & within, most);
+      const int d = 8 * piece_of(x) < dim ? 8 * piece_of(x) : 0;
+      s.at[x] = *(const global_u4 *)((uint64_t)block * bs + ((uint64_t)place * ts + (uint64_t)(from + d)));
     }
     return s;
   };
-  auto stage = [&](int t, Staged &s, uint8_t *to) {
-    const bool drafted = t >= sp.ctx_tiles;
-    const int limit = drafted ? n - (t - sp.ctx_tiles) * TILE : len - t * TILE;
-    // columns past dim are zeros in K; values of keys that there are not become zeros, and so, for now, does what is not
-    // finite in drafted tokens: rows that do not see it must not meet it (0 times infinity)
+  auto request_k = [&](int i, const Pages &p) {
+    return request(i, p, a.c.k + kh * a.c.k_head, a.c.k_block, a.c.k_token, a.b.k + t0 * a.b.k_row + kh * a.b.k_head, a.b.k_row);
+  };
+  auto request_v = [&](int i, const Pages &p) {
+    return request(i, p, a.c.v + kh * a.c.v_head, a.c.v_block, a.c.v_token, a.b.v + t0 * a.b.v_row + kh * a.b.v_head, a.b.v_row);
+  };
+
+  // ... and where it goes in LDS
+  uint8_t *group = lds + wk * (BUFS * 2 * KV);
+  auto k_area = [&](int i) { return group + (BUFS > 1 ? (i & 1) * KV : 0); };
+  auto v_area = [&](int i) { return group + BUFS * KV + (BUFS > 1 ? (i & 1) * KV : 0); };
+  auto put = [&](const Share &s, uint8_t *to) {
+#pragma unroll
+    for (int x = 0; x < LJ; ++x) {
+      if (!there(x)) break;
+      const int key = key_of(x), pc = piece_of(x);
+      *(u4 *)(to + key * ROW + 32 * ((pc >> 1) ^ turn(key)) + 16 * (pc & 1)) = s.at[x];
+    }
+  };
+  auto stage_k = [&](int i, Share s) {                // columns past dim are zeros
     if (dim != 32 * DC)
 #pragma unroll
       for (int x = 0; x < LJ; ++x)
-        if (8 * piece_of(x) >= dim) s.k[x] = u4{0, 0, 0, 0};
+        if (8 * piece_of(x) >= dim) s.at[x] = u4{0, 0, 0, 0};
+    put(s, k_area(i));
+  };
+  // values of keys that there are not become zeros, and so, for now, does what is not finite in drafted tokens: rows
+  // that do not see it must not meet it (0 times infinity)
+  auto stage_v = [&](int i, Share s) {
+    const bool drafted = tile_of(i) >= sp.ctx_tiles;
+    const int limit = limit_of(i);
     if (drafted || limit < TILE) {
       bool odd = false;
 #pragma unroll
       for (int x = 0; x < LJ; ++x) {
         if (!there(x)) break;
-        if (key_of(x) >= limit) s.v[x] = u4{0, 0, 0, 0};
+        if (key_of(x) >= limit) s.at[x] = u4{0, 0, 0, 0};
         if (drafted) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const uint32_t m = odd_halves(s.v[x][e]);
+            const uint32_t m = odd_halves(s.at[x][e]);
             odd |= m != 0;
-            s.v[x][e] &= ~m;
+            s.at[x][e] &= ~m;
           }
         }
       }
       if (odd) odd_seen[wk] = 1;
     }
-#pragma unroll
-    for (int x = 0; x < LJ; ++x) {
-      if (!there(x)) break;
-      const int key = key_of(x), pc = piece_of(x);
-      uint8_t *at = to + key * ROW + 32 * ((pc >> 1) ^ turn(key)) + 16 * (pc & 1);
-      *(u4 *)at = s.k[x];
-      *(u4 *)(at + KV) = s.v[x];
-    }
+    put(s, v_area(i));
   };
 
-  // tiles t, t + WK, ... t + (AHEAD - 1) WK are on their way, the page numbers of the next one too
-  int t = begin + wk;
-  Staged ring[AHEAD];
-  Pages next;
-  {
-    Pages p[AHEAD];
+  // AHEAD tiles are on their way, and the page numbers of AHEAD more.  Which registers they come into is fixed (the loop goes AHEAD
+  // tiles a round): a copy of a register that is still being loaded would wait for it.
+  Share kring[AHEAD], vring[AHEAD];
+  Pages pages[AHEAD];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) p[i] = pages_of(t + i * WK);
-    next = pages_of(t + AHEAD * WK);
+  for (int j = 0; j < AHEAD; ++j) pages[j] = pages_of(j);
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i)
-      if (t + i * WK < end) ring[i] = request(t + i * WK, p[i]);
+  for (int j = 0; j < AHEAD; ++j) {
+    kring[j] = request_k(j, pages[j]);
+    vring[j] = request_v(j, pages[j]);
+    pages[j] = pages_of(j + AHEAD);
   }
+  if (threadIdx.x < W) odd_seen[threadIdx.x] = 0;
 
   // Q^T as the B operand: lane (g, n) holds d = 32 c + 8 g .. + 7 of row n
   h8 q[NR][DC];
@@ -214,109 +226,128 @@ __global__ __launch_bounds__(64 * waves_of(WR), 2) void k_tree(TreeArgs a) {
       q[x][c] = __builtin_bit_cast(h8, v);
     }
   }
-  f4 o[NR][2 * DC];
-  float ref[NR], off[NR], l[NR];                      // reference (base 2), SHIFT - reference, this lane's part of the sum
+  f4 o[NR][2 * DC], l[NR];                            // weighted sums; sums
+  float ref[NR], off[NR];                             // reference (base 2), SHIFT - reference
+  const _Float16 one = 1;
+  const h8 ones = {one, one, one, one, one, one, one, one};
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
     ref[x] = -INFINITY;
-    off[x] = SHIFT;
-    l[x] = 0.f;
+    off[x] = INFINITY;
+    l[x] = f4{0, 0, 0, 0};
 #pragma unroll
     for (int d = 0; d < 2 * DC; ++d) o[x][d] = f4{0, 0, 0, 0};
   }
+
   __syncthreads();                                    // (odd_seen)
 
-  const int steps = (end - begin + WK - 1) / WK;      // (the same for every wave: they meet in a barrier)
-  for (int step = 0; step < steps; ++step, t += WK) {
-    uint8_t *tile = group + (BUFS > 1 ? (step & 1) * 2 * KV : 0);
-    if (t < end) {
-      stage(t, ring[0], tile);
+  auto compute = [&](int i) {
+      const int t = tile_of(i), limit = limit_of(i);
+      const bool drafted = t >= sp.ctx_tiles;
+      f4 s[NR][2];
 #pragma unroll
-      for (int i = 0; i + 1 < AHEAD; ++i) ring[i] = ring[i + 1];
-      if (t + AHEAD * WK < end) ring[AHEAD - 1] = request(t + AHEAD * WK, next);
-      next = pages_of(t + (AHEAD + 1) * WK);
-    }
-    if (WR > 1) lds_barrier();                        // (two buffers: who writes the other one has passed this barrier, and so has every reader)
-    if (t >= end || base >= rows) continue;
-    const bool drafted = t >= sp.ctx_tiles;
-    const int limit = drafted ? n - (t - sp.ctx_tiles) * TILE : len - t * TILE;     // keys of the tile that there are
-    f4 s[NR][2];
+      for (int x = 0; x < NR; ++x) s[x][0] = s[x][1] = f4{0, 0, 0, 0};
 #pragma unroll
-    for (int x = 0; x < NR; ++x) s[x][0] = s[x][1] = f4{0, 0, 0, 0};
+      for (int c = 0; c < DC; ++c)
 #pragma unroll
-    for (int c = 0; c < DC; ++c)
+        for (int h = 0; h < 2; ++h) {
+          const int key = 16 * h + n16;
+          const h8 k = __builtin_bit_cast(h8, *(const u4 *)(k_area(i) + key * ROW + 32 * ((2 * c + (g4 >> 1)) ^ turn(key)) + 16 * (g4 & 1)));
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int key = 16 * h + n16;
-        const h8 k = __builtin_bit_cast(h8, *(const u4 *)(tile + key * ROW + 32 * ((2 * c + (g4 >> 1)) ^ turn(key)) + 16 * (g4 & 1)));
-#pragma unroll
-        for (int x = 0; x < NR; ++x) s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[x][c], s[x][h], 0, 0, 0);
-      }
-    h8 p[NR];
-#pragma unroll
-    for (int x = 0; x < NR; ++x) {
+          for (int x = 0; x < NR; ++x) s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[x][c], s[x][h], 0, 0, 0);
+        }
       if (drafted || limit < TILE) {
-        const int row = base + 16 * x + n16;
-        const uint32_t word = !drafted ? ~0u : row < rows ? (uint32_t)(a.b.mask[t0 + row / a.group] >> ((t - sp.ctx_tiles) * TILE)) : 0u;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int x = 0; x < NR; ++x) {
+          const int row = base + 16 * x + n16;
+          const uint32_t word = !drafted ? ~0u : row < rows ? (uint32_t)(a.b.mask[t0 + row / a.group] >> ((t - sp.ctx_tiles) * TILE)) : 0u;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = 16 * h + 4 * g4 + i;
-            if (key >= limit || !(word >> key & 1)) s[x][h][i] = -INFINITY;
-          }
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int key = 16 * h + 4 * g4 + e;
+              if (key >= limit || !(word >> key & 1)) s[x][h][e] = -INFINITY;
+            }
+        }
       }
-      float top = fmaxf(fmaxf(fmaxf(s[x][0][0], s[x][0][1]), fmaxf(s[x][0][2], s[x][0][3])), fmaxf(fmaxf(s[x][1][0], s[x][1][1]), fmaxf(s[x][1][2], s[x][1][3])));
-      if (__any(top * a.scale2 > ref[x] + SLACK)) {
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64)) * a.scale2;
-        const float to = top > ref[x] + SLACK ? top : ref[x];
-        const float f = ref[x] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[x] - to);     // (nothing is there yet)
-        ref[x] = to;
-        off[x] = to == -INFINITY ? SHIFT : SHIFT - to;
-        l[x] *= f;
+      // Scores that pass the reference too far show in p itself, whose bits order as whole numbers do (no reference yet: off
+      // is infinite, and so is p, or NaN).
+      float e[NR][8];
+      uint32_t most = 0;
 #pragma unroll
-        for (int d = 0; d < 2 * DC; ++d)
+      for (int x = 0; x < NR; ++x)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[x][d][i] *= f;
+        for (int j = 0; j < 8; ++j) {
+          e[x][j] = __builtin_amdgcn_exp2f(fmaf(s[x][j >> 2][j & 3], a.scale2, off[x]));
+          most = max(most, __builtin_bit_cast(uint32_t, e[x][j]));
+        }
+      if (__any(most > __builtin_bit_cast(uint32_t, EXP2_LIMIT))) {
+#pragma unroll
+        for (int x = 0; x < NR; ++x) {
+          float top = fmaxf(fmaxf(fmaxf(s[x][0][0], s[x][0][1]), fmaxf(s[x][0][2], s[x][0][3])), fmaxf(fmaxf(s[x][1][0], s[x][1][1]), fmaxf(s[x][1][2], s[x][1][3])));
+          top = fmaxf(top, __shfl_xor(top, 16, 64));
+          top = fmaxf(top, __shfl_xor(top, 32, 64)) * a.scale2;
+          const float to = top > ref[x] + SLACK ? top : ref[x];
+          const float f = ref[x] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[x] - to);     // (nothing is there yet)
+          ref[x] = to;
+          off[x] = to == -INFINITY ? INFINITY : SHIFT - to;
+          const float now = to == -INFINITY ? SHIFT : off[x];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) l[x][j] *= f;
+#pragma unroll
+          for (int d = 0; d < 2 * DC; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[x][d][j] *= f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) e[x][j] = __builtin_amdgcn_exp2f(fmaf(s[x][j >> 2][j & 3], a.scale2, now));
+        }
       }
-      float e[8];
+      h8 p[NR];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(fmaf(s[x][i >> 2][i & 3], a.scale2, off[x]));
-        p[x][i] = (_Float16)e[i];
+      for (int x = 0; x < NR; ++x)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[x][j] = (_Float16)e[x][j];
+#pragma unroll
+      for (int x = 0; x < NR; ++x) l[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p[x], l[x], 0, 0, 0);      // (every entry of a row: its sum)
+      // V^T as the A operand: lane j of a group of 16 addresses 8 bytes of key 4 g + j / 4, and gets d = 16 dt + n of keys 4 g .. 4 g + 3
+#pragma unroll
+      for (int d = 0; d < 2 * DC; ++d) {
+        u4 v;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int key = 16 * h + 4 * g4 + (n16 >> 2);
+          const u2 both = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(v_area(i) + key * ROW + 32 * (d ^ turn(key)) + 8 * (n16 & 3))));
+          v[2 * h] = both.x;
+          v[2 * h + 1] = both.y;
+        }
+#pragma unroll
+        for (int x = 0; x < NR; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, v), p[x], o[x][d], 0, 0, 0);
       }
-      l[x] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+  };
+#pragma unroll 1
+  for (int i = 0; i < steps; i += AHEAD)
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (i + j >= steps) break;
+      stage_k(i + j, kring[j]);
+      stage_v(i + j, vring[j]);
+      kring[j] = request_k(i + j + AHEAD, pages[j]);
+      vring[j] = request_v(i + j + AHEAD, pages[j]);
+      pages[j] = pages_of(i + j + 2 * AHEAD);
+      if (WR > 1) lds_barrier();                      // (two buffers: who writes the other one has passed this barrier, and so has every reader)
+      if (busy) compute(i + j);
     }
-    // lane j of a group of 16 addresses 8 bytes of key 4 g + j / 4, and gets d = 16 dt + n of keys 4 g .. 4 g + 3
-#pragma unroll
-    for (int d = 0; d < 2 * DC; ++d) {
-      u4 v;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int key = 16 * h + 4 * g4 + (n16 >> 2);
-        const s4v w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(tile + KV + key * ROW + 32 * (d ^ turn(key)) + 8 * (n16 & 3)));
-        const u2 both = __builtin_bit_cast(u2, w);
-        v[2 * h] = both.x;
-        v[2 * h + 1] = both.y;
-      }
-#pragma unroll
-      for (int x = 0; x < NR; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, v), p[x], o[x][d], 0, 0, 0);
-    }
-  }
 
   // the waves over the keys join: references and sums, then the weighted sums a row tile at a time through the V areas
   __shared__ float refs[W][16 * NR], sums[W][16 * NR];
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
-    l[x] += __shfl_xor(l[x], 16, 64);
-    l[x] += __shfl_xor(l[x], 32, 64);
     if (g4 == 0) {
       refs[wave][16 * x + n16] = ref[x];
-      sums[wave][16 * x + n16] = l[x];
+      sums[wave][16 * x + n16] = l[x][0];
     }
   }
-  bad = __syncthreads_or(bad);
+  const bool bad = __syncthreads_or(a.c.blocks > 0 && worst >= (uint32_t)a.c.blocks);
   if (odd_seen[wk] && base < rows) {                  // (rare) what is not finite in drafted tokens, to the rows that see it
     const int first = max(begin, sp.ctx_tiles);
     for (int key = 0; key < min((end - sp.ctx_tiles) * TILE, n); ++key) {
@@ -461,7 +492,7 @@ struct Shape { int nr, wr, row_blocks, splits, min_tiles; };
 Shape shape_of(const egt_tree_batch &b, const egt_kv_cache &c) {
   Shape s;
   const int rows = b.max_tokens * (b.heads / c.heads);
-  s.nr = rows <= 16 || c.dim > 128 ? 1 : 2;
+  s.nr = rows <= 64 || c.dim > 128 ? 1 : 2;
   s.wr = 1;
   while (s.wr < 8 && rows > 16 * s.nr * s.wr) s.wr *= 2;
   s.row_blocks = (rows + 16 * s.nr * s.wr - 1) / (16 * s.nr * s.wr);
@@ -488,14 +519,16 @@ hipError_t launch_tree(const TreeArgs &a, hipStream_t stream) {
 }
 template <int DC>
 hipError_t launch_dim(const TreeArgs &a, const Shape &s, hipStream_t stream) {
-  constexpr int NR = DC <= 4 ? 2 : 1;
-  if (s.nr == 1 && s.wr == 1) return launch_tree<DC, 1, 1>(a, stream);
+  if constexpr (DC <= 4)
+    if (s.nr == 2) return s.wr == 4 ? launch_tree<DC, 2, 4>(a, stream) : launch_tree<DC, 2, 8>(a, stream);
   switch (s.wr) {
-    case 1: return launch_tree<DC, NR, 1>(a, stream);
-    case 2: return launch_tree<DC, NR, 2>(a, stream);
-    case 4: return launch_tree<DC, NR, 4>(a, stream);
-    default: return launch_tree<DC, NR, 8>(a, stream);
+    case 1: return launch_tree<DC, 1, 1>(a, stream);
+    case 2: return launch_tree<DC, 1, 2>(a, stream);
+    case 4: return launch_tree<DC, 1, 4>(a, stream);
+    default: break;
   }
+  if constexpr (DC > 4) return launch_tree<DC, 1, 8>(a, stream);
+  return hipErrorInvalidValue;                        // (not reached: shape_of takes no other)
 }
 
 }  // namespace
@@ -516,6 +549,7 @@ egt_status egt_tree_attention(const egt_tree_batch *b, const egt_kv_cache *cache
   st = egt::check_cache(cache, true);
   if (st != EGT_OK) return st;
   if (b->ld_table < b->table_blocks || !(b->scale == b->scale)) return EGT_ERR_SHAPE;
+  if (std::max({cache->k_block, cache->v_block, cache->k_token, cache->v_token, b->k_row, b->v_row}) >= 1ll << 31) return EGT_ERR_UNSUPPORTED;
   if (b->requests == 0 || b->tokens == 0) return EGT_OK;
   if (!b->q || !b->k || !b->v || !b->out || !b->lens || !b->cu_tokens || !b->mask || (b->table_blocks && !b->block_table) || !workspace) return EGT_ERR_NULL;
   if (workspace_bytes < egt::workspace_of(*b, *cache)) return EGT_ERR_SHAPE;
