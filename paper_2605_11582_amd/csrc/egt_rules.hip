@@ -1,79 +1,184 @@
 // Penalties for repeated tokens, biases and grammar masks on logits.
+//
+// One pass over the logits; what makes it more than a copy is that a row's history says something about a few thousand of a hundred
+// thousand ids.  A workgroup takes a slice of the vocabulary and some rows: for every request among them it counts the history's ids that
+// fall into the slice in LDS - whole numbers, so that the order of the atomics does not show - and its waves then pass over the
+// rows, 8 ids a lane, each with its count at hand.  The drafted tokens that a row sees differ from row to row: their ids, few in a
+// slice, are done again after the pass by the lanes that stand for them.  Bound by the logits' bytes, and for a single row by a
+// launch and the chain cu_tokens - lengths - history - logits.
+#include "egt_mfma_common.h"
 #include "egt_serve.h"
+
+#include <algorithm>
 
 namespace egt {
 namespace {
 
-constexpr int SLICE = 4096;              // ids a workgroup looks at
-constexpr uint32_t PROMPT = 1u << 31;    // in a counter: the id is in the prompt
+// A counter: how often the id is written, whether it is in the prompt, whether a bias names it.
+constexpr uint32_t PROMPT = 1u << 31, NAMED = 1u << 30, COUNT = NAMED - 1;
 
+// 8 logits, at any address that suits one
 template <typename T>
-__device__ __forceinline__ void put(T *p, float v);
-template <>
-__device__ __forceinline__ void put(float *p, float v) { *p = v; }
-template <>
-__device__ __forceinline__ void put(__half *p, float v) { *p = __float2half(v); }
+struct __attribute__((packed, aligned(sizeof(T)))) Eight { T v[8]; };
 
-// The request of a row: the last one that starts at the row or before; -1 where the row is nobody's.
+__device__ __forceinline__ float wide(__half v) { return (float)v; }
+__device__ __forceinline__ float wide(float v) { return v; }
+__device__ __forceinline__ void narrow(__half &o, float v) { o = __float2half(v); }
+__device__ __forceinline__ void narrow(float &o, float v) { o = v; }
+
+// The request of a row: the last one that starts at the row or before; -1 where the row is nobody's.  All lanes look at once,
+// 64 places a round.
 __device__ __forceinline__ int request_of(const int32_t *cu, int n, int rows, int row) {
-  int r = -1;
-  for (int lo = 0, hi = n; lo < hi;) {
-    const int mid = (lo + hi) >> 1;
-    if (cu[mid] <= row) { r = mid; lo = mid + 1; } else { hi = mid; }
+  const int lane = threadIdx.x & 63;
+  int lo = 0;
+  while (n > 1) {
+    const int step = (n + 63) / 64, at = lane * step;
+    const uint64_t before = __ballot(at < n && cu[lo + min(at, n - 1)] <= row);
+    if (!before) return -1;
+    const int k = 63 - __builtin_clzll(before);
+    lo += k * step;
+    n = min(step, n - k * step);
   }
-  if (r < 0 || cu[r] < 0 || cu[r + 1] <= row || cu[r + 1] > rows) return -1;
-  return r;
+  const int t0 = cu[lo], t1 = cu[lo + 1];
+  return t0 >= 0 && t0 <= row && row < t1 && t1 <= rows ? lo : -1;
 }
 
-// A workgroup is one row and SLICE ids: it counts the row's history that falls among them in LDS - whole numbers, so that the
-// order of the atomics does not show - and then passes over the logits once.
-template <typename T>
-__global__ __launch_bounds__(256) void k_logits_rules(egt_rules_batch b) {
-  __shared__ uint32_t count[SLICE], named[SLICE];
-  const int row = blockIdx.y, tid = threadIdx.x, first = blockIdx.x * SLICE, ids = min(SLICE, b.vocab - first);
-  const int r = request_of(b.cu_tokens, b.requests, b.tokens, row);
-  if (r < 0) return;
-  for (int t = tid; t < SLICE; t += 256) count[t] = named[t] = 0;
-  __syncthreads();
-  if (b.history) {
-    const int32_t *h = b.history + r * b.ld_history;
-    const int n = min(max(b.history_len[r], 0), b.history_width), told = b.prompt_len ? min(max(b.prompt_len[r], 0), n) : 0;
-    for (int i = tid; i < n; i += 256) {
-      const uint32_t t = (uint32_t)(h[i] - first);
-      if (t < (uint32_t)ids && h[i] >= 0) {
-        if (i < told) atomicOr(&count[t], PROMPT); else atomicAdd(&count[t], 1u);
+struct Rules {
+  float repetition, frequency, presence;
+  const int32_t *bias_ids;
+  const float *bias;
+  int n_bias;
+};
+// The rules in their order, but for the grammar's.
+__device__ __forceinline__ float apply(const egt_rules_batch &b, const Rules &u, float x, uint32_t n, int id) {
+  if (n & ~NAMED && b.repetition) x = x > 0.f ? x / u.repetition : x * u.repetition;
+  if (n & COUNT) {
+    x = x - u.frequency * (float)(n & COUNT);
+    x = x - u.presence;
+  }
+  if (n & NAMED) {                                    // (few ids are: the list is looked through for them alone)
+    float add = 0.f;
+    for (int i = 0; i < u.n_bias; ++i)
+      if (u.bias_ids[i] == id) add = u.bias[i];
+    x = x + add;
+  }
+  return x;
+}
+
+template <typename T, int SLICE>
+__global__ __launch_bounds__(256) void k_logits_rules(egt_rules_batch b, int rows_each) {
+  __shared__ uint32_t count[SLICE];
+  constexpr int PART = SLICE / 4;                     // what a wave takes of a row at a time
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int first = blockIdx.x * SLICE, ids = min(SLICE, b.vocab - first), stop = min((int)(blockIdx.y + 1) * rows_each, b.tokens);
+  for (int row = blockIdx.y * rows_each; row < stop;) {
+    const int r = request_of(b.cu_tokens, b.requests, b.tokens, row);
+    if (r < 0) {
+      ++row;
+      continue;
+    }
+    const int t0 = b.cu_tokens[r], t1 = b.cu_tokens[r + 1], end = min(t1, stop);
+    // ---- what the request's history and biases say about this slice
+    for (int t = 4 * tid; t < SLICE; t += 1024) *(uint4 *)(count + t) = uint4{0, 0, 0, 0};
+    __syncthreads();
+    if (b.history) {
+      const int32_t *h = b.history + r * b.ld_history;
+      const int n = min(max(b.history_len[r], 0), b.history_width), told = b.prompt_len ? min(max(b.prompt_len[r], 0), n) : 0;
+      auto take = [&](int i, int id) {
+        const uint32_t t = (uint32_t)id - (uint32_t)first;
+        if (t < (uint32_t)ids) {
+          if (i < told) atomicOr(&count[t], PROMPT); else atomicAdd(&count[t], 1u);
+        }
+      };
+      const int whole = ((uintptr_t)h & 15) == 0 ? n & ~3 : 0;
+      for (int i = 4 * tid; i < whole; i += 1024) {
+        const int4 v = *(const int4 *)(h + i);
+        take(i, v.x), take(i + 1, v.y), take(i + 2, v.z), take(i + 3, v.w);
+      }
+      for (int i = whole + tid; i < n; i += 256) take(i, h[i]);
+    }
+    Rules u;
+    u.bias_ids = b.bias_ids ? b.bias_ids + (int64_t)r * b.n_bias : nullptr;
+    u.bias = b.bias_ids ? b.bias + (int64_t)r * b.n_bias : nullptr;
+    u.n_bias = b.bias_ids ? b.n_bias : 0;
+    for (int i = tid; i < u.n_bias; i += 256) {
+      const uint32_t t = (uint32_t)u.bias_ids[i] - (uint32_t)first;
+      if (t < (uint32_t)ids) atomicOr(&count[t], NAMED);
+    }
+    u.repetition = b.repetition ? b.repetition[r] : 1.f;
+    u.frequency = b.frequency ? b.frequency[r] : 0.f;
+    u.presence = b.presence ? b.presence[r] : 0.f;
+    // the drafted token that this lane stands for (a row sees those whose bits are set)
+    const int mates = min(t1 - t0, 64);
+    const int draft = b.draft && lane < mates ? b.draft[t0 + lane] : -1;
+    __syncthreads();
+
+    // ---- the rows, a quarter of the slice at a time
+    for (int unit = 4 * row + wave; unit < 4 * end; unit += 4) {
+      const int i = unit >> 2, from = (unit & 3) * PART, to = min(from + PART, ids);
+      if (from >= to) continue;
+      const T *x = (const T *)b.logits + i * b.ld_logits + first;
+      T *y = (T *)b.out + i * b.ld_out + first;
+      const int which = b.allowed ? b.allowed_row[i] : -1;
+      const bool broken = b.allowed && which >= b.n_allowed;
+      const uint32_t *allowed = which >= 0 && !broken ? b.allowed + which * b.ld_allowed + first / 32 : nullptr;
+      const bool seen = b.draft && draft >= first + from && draft < first + to && (b.mask[i] >> lane & 1);
+      const uint64_t some = __ballot(seen);
+      float again = 0.f;
+      if (some) {                                     // (read before the pass, which may be in place)
+        uint32_t times = 0;
+        for (uint64_t left = some; left; left &= left - 1) {
+          const int o = __builtin_ctzll(left);
+          const bool same = __builtin_amdgcn_readlane(draft, o) == draft;
+          times += same;
+        }
+        if (seen) {
+          const int t = draft - first;
+          again = apply(b, u, wide(x[t]), count[t] + times, draft);
+          if (broken) again = __builtin_nanf("");
+          else if (allowed && !(allowed[t >> 5] >> (t & 31) & 1)) again = -INFINITY;
+        }
+      }
+      for (int t = from + 8 * lane; t < to; t += 512) {
+        const uint32_t bits = allowed ? allowed[t >> 5] >> (t & 31) : ~0u;
+        Eight<T> v;
+        const int n = to - t;
+        if (n >= 8) {
+          v = *(const Eight<T> *)(x + t);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e < n) v.v[e] = x[t + e];
+        }
+        const uint4 c0 = *(const uint4 *)(count + t), c1 = *(const uint4 *)(count + t + 4);
+        const uint32_t c[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+        const uint32_t any = (c0.x | c0.y | c0.z | c0.w) | (c1.x | c1.y | c1.z | c1.w);
+        // (most ids have no history: theirs are passed on as they are)
+        if (any || (bits & 0xff) != 0xff || broken) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float z = wide(v.v[e]);
+            if (c[e]) z = apply(b, u, z, c[e], first + t + e);
+            if (broken) z = __builtin_nanf("");
+            else if (!(bits >> e & 1)) z = -INFINITY;
+            narrow(v.v[e], z);
+          }
+        }
+        if (n >= 8) {
+          *(Eight<T> *)(y + t) = v;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e < n) y[t + e] = v.v[e];
+        }
+      }
+      if (some) {
+        wait_vmem<0>();                               // (the pass has written these ids too)
+        if (seen) narrow(y[draft - first], again);    // (tokens of one id write the same number)
       }
     }
-  }
-  if (b.draft) {
-    const int t0 = b.cu_tokens[r], n = min(b.cu_tokens[r + 1] - t0, 64);
-    if (tid < n && (b.mask[row] >> tid & 1)) {
-      const int id = b.draft[t0 + tid];
-      if (id >= first && id < first + ids) atomicAdd(&count[id - first], 1u);
-    }
-  }
-  if (b.bias_ids)
-    for (int i = tid; i < b.n_bias; i += 256) {
-      const int id = b.bias_ids[(int64_t)r * b.n_bias + i];
-      if (id >= first && id < first + ids) atomicMax(&named[id - first], (uint32_t)i + 1);
-    }
-  __syncthreads();
-  const float rep = b.repetition ? b.repetition[r] : 1.f, freq = b.frequency ? b.frequency[r] : 0.f, pres = b.presence ? b.presence[r] : 0.f;
-  const int which = b.allowed ? b.allowed_row[row] : -1;
-  const T *x = (const T *)b.logits + row * b.ld_logits + first;
-  T *y = (T *)b.out + row * b.ld_out + first;
-  for (int t = tid; t < ids; t += 256) {
-    float v = (float)x[t];
-    const uint32_t n = count[t];
-    if (n && b.repetition) v = v > 0.f ? v / rep : v * rep;
-    if (n & ~PROMPT) {
-      v = v - freq * (float)(n & ~PROMPT);
-      v = v - pres;
-    }
-    if (named[t]) v = v + b.bias[(int64_t)r * b.n_bias + named[t] - 1];
-    if (which >= b.n_allowed && b.allowed) v = __builtin_nanf("");
-    else if (which >= 0 && !(b.allowed[which * b.ld_allowed + ((first + t) >> 5)] >> ((first + t) & 31) & 1)) v = -INFINITY;
-    put(y + t, v);
+    row = end;
+    __syncthreads();                                  // (the counters are cleared next)
   }
 }
 
@@ -88,7 +193,7 @@ egt_status egt_logits_rules(const egt_rules_batch *b, void *stream) {
       b->ld_logits < b->vocab || b->ld_out < b->vocab || b->history_width < 0 || (b->history && b->ld_history < b->history_width) || b->ld_allowed < 0 || (b->allowed && b->ld_allowed < ((int64_t)b->vocab + 31) / 32) ||
       (b->logits == b->out && b->ld_logits != b->ld_out))
     return EGT_ERR_SHAPE;
-  if (b->requests > EGT_MAX_REQUESTS || b->tokens > 65535) return EGT_ERR_UNSUPPORTED;
+  if (b->requests > EGT_MAX_REQUESTS || b->tokens > 65535 || b->vocab > (1 << 30)) return EGT_ERR_UNSUPPORTED;
   if (b->requests == 0 || b->tokens == 0 || b->vocab == 0) return EGT_OK;
   if (!b->logits || !b->out || !b->cu_tokens || (b->history && !b->history_len) || (b->draft && !b->mask) || (b->bias_ids && !b->bias) ||
       (b->allowed && !b->allowed_row))
@@ -99,9 +204,19 @@ egt_status egt_logits_rules(const egt_rules_batch *b, void *stream) {
                         (const void *)b->repetition, (const void *)b->frequency, (const void *)b->presence, (const void *)b->bias_ids, (const void *)b->bias,
                         (const void *)b->allowed, (const void *)b->allowed_row})
     if ((uintptr_t)p & 3) return EGT_ERR_BUFFER;
-  const dim3 grid((unsigned)((b->vocab + egt::SLICE - 1) / egt::SLICE), (unsigned)b->tokens);
-  auto *kernel = b->kind == EGT_LOGITS_FP16 ? egt::k_logits_rules<__half> : egt::k_logits_rules<float>;
-  return egt::answer(egt::launch(kernel, grid, dim3(256), 0, (hipStream_t)stream, *b));
+  // Slices of 4096 ids count a history in fewer workgroups; where rows are few, slices of 1024 have the whole chip at work.  Rows of one
+  // request share a count: as many together as a request has on average, as long as there are workgroups for the chip.
+  const bool large = (int64_t)b->tokens * ((b->vocab + 4095) / 4096) >= 512;
+  const int slices = large ? (b->vocab + 4095) / 4096 : (b->vocab + 1023) / 1024;
+  const int64_t each = std::min<int64_t>((int64_t)b->tokens * slices / 512, (b->tokens + b->requests - 1) / b->requests);
+  const int rows_each = (int)std::min<int64_t>(std::max<int64_t>(each, 1), 64);
+  const dim3 grid((unsigned)slices, (unsigned)((b->tokens + rows_each - 1) / rows_each)), block(256);
+  const hipStream_t to = (hipStream_t)stream;
+  if (b->kind == EGT_LOGITS_FP16)
+    return egt::answer(large ? egt::launch(egt::k_logits_rules<__half, 4096>, grid, block, 0, to, *b, rows_each)
+                             : egt::launch(egt::k_logits_rules<__half, 1024>, grid, block, 0, to, *b, rows_each));
+  return egt::answer(large ? egt::launch(egt::k_logits_rules<float, 4096>, grid, block, 0, to, *b, rows_each)
+                           : egt::launch(egt::k_logits_rules<float, 1024>, grid, block, 0, to, *b, rows_each));
 }
 
 }  // extern "C"
