@@ -9,70 +9,91 @@ namespace {
 
 constexpr int SLOT_THREADS = 256;
 
-// Sum of `v` over the threads before this one.  `part`: one word a wave; all threads of the workgroup call it.
-__device__ __forceinline__ int64_t sum_before(int64_t v, int64_t *part) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t s = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t t = __shfl_up(s, o, 64);
-    if (lane >= o) s += t;
-  }
-  if (lane == 63) part[wave] = s;
+// Sums are held to what fits 31 bits: the order of additions does not matter to them, and a sum that is held is too large for
+// anything it is compared with.
+constexpr uint32_t MOST = INT32_MAX;
+__device__ __forceinline__ uint32_t held(uint32_t a, uint32_t b) { return min(a + b, MOST); }
+
+// Sum over the lanes up to this one, within a row of 16 and then across rows.
+__device__ __forceinline__ uint32_t sum_upto(uint32_t v) {
+  v = held(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));      // row_shr:1, 2, 4, 8
+  v = held(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
+  v = held(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
+  v = held(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
+  v = held(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));      // row_bcast:15 into rows 1 and 3
+  v = held(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));      // row_bcast:31 into rows 2 and 3
+  return v;
+}
+// Sum over the threads before this one, or, for one wave's requests, over its lanes: then every wave has all of them and nobody waits.
+template <bool ONE>
+__device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t *part) {
+  const uint32_t upto = sum_upto(v);
+  uint32_t before = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)upto, 0x138, 0xf, 0xf, false);      // wave_shr:1
+  if (ONE) return before;
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 63) part[wave] = upto;
   __syncthreads();
-  int64_t before = s - v;
-  for (int w = 0; w < wave; ++w) before += part[w];
+  uint32_t waves = 0;
+  for (int w = 0; w < wave; ++w) waves = held(waves, part[w]);
   __syncthreads();                                    // (part is used again)
-  return before;
+  return held(waves, before);
 }
 
 // Two running sums over the requests - tokens, then pages - decide everything, and a few thousand lengths are 16 KB: every
-// workgroup computes both for itself (each thread a run of requests, then one scan over the threads) and keeps them in LDS, so
-// that the token slots, which are the bytes, are written by the whole chip without a second launch and without one workgroup
-// waiting for another.  What binds it is that chain: two loads, two scans, a search, a page number.
+// workgroup computes both for itself (each thread a run of requests, then one scan over the threads; up to 64 requests every wave
+// for itself, a lane a request) and keeps them in LDS, so that the token slots, which are the bytes, are written by the whole chip
+// without a second launch and without one workgroup waiting for another.  What binds it is that chain: lengths, two scans, a
+// search, a page number, behind a launch.
+template <bool ONE>
 __global__ __launch_bounds__(SLOT_THREADS) void k_kv_slots(egt_slots_batch b, int shift) {
   extern __shared__ int32_t lds[];
-  __shared__ int64_t part[SLOT_THREADS / 64];
+  __shared__ uint32_t part[SLOT_THREADS / 64];
   const int n = b.requests, tid = threadIdx.x;
   int32_t *cu = lds, *first = lds + n + 1;            // first token; first free page (-1: the request gets nothing)
-  const int per = (n + SLOT_THREADS - 1) / SLOT_THREADS;
-  const int r0 = min(tid * per, n), r1 = min(r0 + per, n);
-  int64_t tokens = 0;
-  for (int r = r0; r < r1; ++r) tokens += max(b.counts[r], 0);
-  int64_t at = sum_before(tokens, part), pages = 0;
-  for (int r = r0; r < r1; ++r) {
-    const int64_t len = b.lens[r], c = b.counts[r], end = at + max(c, (int64_t)0);
-    const bool room = len >= 0 && c >= 0 && len + c <= (int64_t)b.table_blocks << shift && end <= b.n_slots;
-    const int64_t up = (1 << shift) - 1, need = room ? ((len + c + up) >> shift) - ((len + up) >> shift) : 0;
-    cu[r] = (int32_t)min(at, (int64_t)b.n_slots);
-    first[r] = room ? (int32_t)need : -1;
-    at = end;
-    pages += need;
-  }
-  if (r0 < r1 && r1 == n) cu[n] = (int32_t)min(at, (int64_t)b.n_slots);
+  const int per = ONE ? 1 : (n + SLOT_THREADS - 1) / SLOT_THREADS;
+  const int r0 = min((ONE ? tid & 63 : tid) * per, n), r1 = min(r0 + per, n);
   const int head = *b.free_head;
-  const int64_t left = head >= 0 ? max((int64_t)b.n_free - head, (int64_t)0) : 0;
-  int64_t start = sum_before(pages, part), top = 0;
+  const int len0 = r0 < r1 ? b.lens[r0] : 0, count0 = r0 < r1 ? b.counts[r0] : 0;
+  uint32_t tokens = (uint32_t)max(count0, 0);
+  for (int r = r0 + 1; r < r1; ++r) tokens = held(tokens, (uint32_t)max(b.counts[r], 0));
+  uint32_t at = sum_before<ONE>(tokens, part), pages = 0;
+  int need0 = -1;
   for (int r = r0; r < r1; ++r) {
-    const int need = first[r];
-    if (need <= 0) continue;                          // (no page needed: kept, at 0; refused already: -1)
-    start += need;
-    first[r] = start <= left ? (int32_t)(start - need) : -1;
-    if (start <= left) top = start;
+    const int64_t len = r == r0 ? len0 : b.lens[r], c = r == r0 ? count0 : b.counts[r];
+    const uint32_t end = held(at, (uint32_t)max(c, (int64_t)0));
+    const bool room = len >= 0 && c >= 0 && len + c <= (int64_t)b.table_blocks << shift && end <= (uint32_t)b.n_slots && end < MOST;
+    const int64_t up = (1 << shift) - 1, need = room ? ((len + c + up) >> shift) - ((len + up) >> shift) : 0;
+    cu[r] = (int32_t)min(at, (uint32_t)b.n_slots);
+    need0 = room ? (int32_t)need : -1;
+    if (!ONE) first[r] = need0;                       // (kept there until the second scan is done)
+    at = end;
+    pages = held(pages, (uint32_t)need);
   }
-  __syncthreads();
+  if (r0 < r1 && r1 == n) cu[n] = (int32_t)min(at, (uint32_t)b.n_slots);
+  const uint32_t left = head >= 0 ? (uint32_t)max(b.n_free - head, 0) : 0;
+  uint32_t start = sum_before<ONE>(pages, part), top = 0;
+  for (int r = r0; r < r1; ++r) {
+    // (ONE: every wave writes each entry once, and all write the same: none reads another's half-done work)
+    const int need = ONE ? need0 : first[r];
+    start = held(start, (uint32_t)max(need, 0));
+    const bool fits = start <= left && start < MOST;
+    first[r] = need <= 0 ? need : fits ? (int32_t)(start - need) : -1;      // (no page needed: 0; refused already: -1)
+    if (need > 0 && fits) top = start;
+  }
+  if (!ONE) __syncthreads();
 
   if (blockIdx.x == 0) {
     for (int r = tid; r <= n; r += SLOT_THREADS) b.cu_tokens[r] = cu[r];
     for (int r = tid; r < n; r += SLOT_THREADS) b.new_lens[r] = b.lens[r] + (first[r] >= 0 ? b.counts[r] : 0);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
-    if ((tid & 63) == 0) part[tid >> 6] = top;
-    __syncthreads();
-    if (tid == 0) {
-      for (int w = 1; w < SLOT_THREADS / 64; ++w) top = max(top, part[w]);
-      *b.new_head = head + (int32_t)top;
+    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    if (!ONE) {
+      if ((tid & 63) == 0) part[tid >> 6] = top;
+      __syncthreads();
+      if (tid == 0)
+        for (int w = 1; w < SLOT_THREADS / 64; ++w) top = max(top, part[w]);
     }
+    if (tid == 0) *b.new_head = head + (int32_t)top;
   }
   // the pages that are taken: a wave a request
   const int waves = gridDim.x * (SLOT_THREADS / 64);
@@ -152,7 +173,9 @@ egt_status egt_kv_slots(const egt_slots_batch *b, void *stream) {
   if (b->lens == b->new_lens || b->counts == b->new_lens || b->free_head == b->new_head) return EGT_ERR_BUFFER;
   const int64_t want = ((int64_t)b->n_slots + 4 * egt::SLOT_THREADS - 1) / (4 * egt::SLOT_THREADS);
   const dim3 grid((unsigned)std::min<int64_t>(std::max<int64_t>(want, 1), 512)), block(egt::SLOT_THREADS);
-  return egt::answer(egt::launch(egt::k_kv_slots, grid, block, 4 * (size_t)(2 * b->requests + 1), (hipStream_t)stream, *b, egt::log2_of(b->page)));
+  const size_t lds = 4 * (size_t)(2 * b->requests + 1);
+  return egt::answer(b->requests <= 64 ? egt::launch(egt::k_kv_slots<true>, grid, block, lds, (hipStream_t)stream, *b, egt::log2_of(b->page))
+                                       : egt::launch(egt::k_kv_slots<false>, grid, block, lds, (hipStream_t)stream, *b, egt::log2_of(b->page)));
 }
 
 egt_status egt_kv_append(const egt_append_batch *b, const egt_kv_cache *cache, void *stream) {

@@ -213,8 +213,11 @@ __global__ __launch_bounds__(256) void k_lora_expand(egt_lora_batch b, const flo
 
 template <int RC>
 hipError_t launch_expand(const egt_lora_batch &b, const float *part, int slices, hipStream_t stream) {
-  // row tiles a wave: four where that leaves two workgroups a compute unit if every token has an adapter of its own
+  // row tiles a wave: more where there are plenty of rows if every token has an adapter of its own (the workgroups of tokens that
+  // another one speaks for are launched too)
   const int64_t groups = (int64_t)((b.rows + 63) / 64) * std::min(b.M, b.adapters);
+  if constexpr (RC < 4)
+    if (groups >= 4096) return launch(k_lora_expand<RC, 8>, dim3((b.rows + 511) / 512, b.M), dim3(256), 0, stream, b, part, slices);
   if (groups >= 2048) return launch(k_lora_expand<RC, 4>, dim3((b.rows + 255) / 256, b.M), dim3(256), 0, stream, b, part, slices);
   return launch(k_lora_expand<RC, 1>, dim3((b.rows + 63) / 64, b.M), dim3(256), 0, stream, b, part, slices);
 }

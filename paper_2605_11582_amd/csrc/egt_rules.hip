@@ -3,8 +3,8 @@
 // One pass over the logits; what makes it more than a copy is that a row's history says something about a few thousand of a hundred
 // thousand ids.  A workgroup takes a slice of the vocabulary and some rows: for every request among them it counts the history's ids that
 // fall into the slice in LDS - whole numbers, so that the order of the atomics does not show - and its waves then pass over the
-// rows, 8 ids a lane, each with its count at hand.  The drafted tokens that a row sees differ from row to row: their ids, few in a
-// slice, are done again after the pass by the lanes that stand for them.  Bound by the logits' bytes, and for a single row by a
+// rows, 8 ids a lane, each with its count at hand, the next row's logits on their way.  The drafted tokens that a row sees differ
+// from row to row: their ids, few in a slice, are done again after the pass by the lanes that stand for them.  Bound by the logits' bytes, and for a single row by a
 // launch and the chain cu_tokens - lengths - history - logits.
 #include "egt_mfma_common.h"
 #include "egt_serve.h"
@@ -43,43 +43,78 @@ __device__ __forceinline__ int request_of(const int32_t *cu, int n, int rows, in
   return t0 >= 0 && t0 <= row && row < t1 && t1 <= rows ? lo : -1;
 }
 
+// What a request has the rules say.
 struct Rules {
-  float repetition, frequency, presence;
+  float repetition, back, frequency, presence;        // back: 1 / repetition (a quotient is a product with it: one rounding more)
   const int32_t *bias_ids;
   const float *bias;
   int n_bias;
 };
-// The rules in their order, but for the grammar's.
-__device__ __forceinline__ float apply(const egt_rules_batch &b, const Rules &u, float x, uint32_t n, int id) {
-  if (n & ~NAMED && b.repetition) x = x > 0.f ? x / u.repetition : x * u.repetition;
-  if (n & COUNT) {
-    x = x - u.frequency * (float)(n & COUNT);
-    x = x - u.presence;
-  }
-  if (n & NAMED) {                                    // (few ids are: the list is looked through for them alone)
-    float add = 0.f;
-    for (int i = 0; i < u.n_bias; ++i)
-      if (u.bias_ids[i] == id) add = u.bias[i];
-    x = x + add;
-  }
-  return x;
+// The penalties, in their order, of an id with the counter `n`.
+__device__ __forceinline__ float penalised(const Rules &u, float x, uint32_t n) {
+  const float f = (float)(n & COUNT);
+  float y = n & ~NAMED ? x * (x > 0.f ? u.back : u.repetition) : x;
+  const float z = (y - u.frequency * f) - u.presence;
+  return n & COUNT ? z : y;
 }
-
 template <typename T, int SLICE>
 __global__ __launch_bounds__(256) void k_logits_rules(egt_rules_batch b, int rows_each) {
-  __shared__ uint32_t count[SLICE];
-  constexpr int PART = SLICE / 4;                     // what a wave takes of a row at a time
+  // a wave takes a quarter of the slice: VL times 8 ids a lane
+  constexpr int PART = SLICE / 4, VL = PART / 512 > 0 ? PART / 512 : 1;
+  __shared__ uint32_t count[SLICE], named[SLICE];     // a counter for each id; one more than the last entry of the bias list that names it
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int first = blockIdx.x * SLICE, ids = min(SLICE, b.vocab - first), stop = min((int)(blockIdx.y + 1) * rows_each, b.tokens);
-  for (int row = blockIdx.y * rows_each; row < stop;) {
-    const int r = request_of(b.cu_tokens, b.requests, b.tokens, row);
-    if (r < 0) {
-      ++row;
-      continue;
+  const int from = wave * PART, to = min(from + PART, ids);      // (nothing where from >= to)
+
+  // What is there of a row before anything is known of its request: its logits, and what its grammar allows.
+  struct Row { Eight<T> v[VL]; uint32_t bits[VL]; bool broken; };
+  auto fetch = [&](int row) {
+    Row w;
+    const int i = min(row, stop - 1);
+    const int which = b.allowed ? b.allowed_row[i] : -1;
+    w.broken = b.allowed && which >= b.n_allowed;
+    const uint32_t *allowed = which >= 0 && !w.broken ? b.allowed + which * b.ld_allowed + first / 32 : nullptr;
+    const T *x = (const T *)b.logits + i * b.ld_logits + first;
+#pragma unroll
+    for (int q = 0; q < VL; ++q) {
+      const int t = from + 512 * q + 8 * lane;
+      w.bits[q] = ~0u;
+      if (t < to) {
+        if (allowed) w.bits[q] = allowed[t >> 5];
+        if (t + 8 <= to) {
+          w.v[q] = *(const Eight<T> *)(x + t);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (t + e < to) w.v[q].v[e] = x[t + e];
+        }
+      }
     }
-    const int t0 = b.cu_tokens[r], t1 = b.cu_tokens[r + 1], end = min(t1, stop);
-    // ---- what the request's history and biases say about this slice
-    for (int t = 4 * tid; t < SLICE; t += 1024) *(uint4 *)(count + t) = uint4{0, 0, 0, 0};
+    return w;
+  };
+
+  int r = -1, t0 = 0, end = blockIdx.y * rows_each, draft = -1;      // the request at hand ends before row `end`
+  Rules u;
+  auto turn_to = [&](int row) {
+    __syncthreads();                                  // (the counters of the last request are read no more)
+    r = request_of(b.cu_tokens, b.requests, b.tokens, row);
+    end = row + 1;
+    if (r < 0) return;
+    t0 = b.cu_tokens[r];
+    end = b.cu_tokens[r + 1];
+    const int mates = min(end - t0, 64);
+    for (int t = 4 * tid; t < SLICE; t += 1024) {
+      *(uint4 *)(count + t) = uint4{0, 0, 0, 0};
+      if (b.bias_ids) *(uint4 *)(named + t) = uint4{0, 0, 0, 0};
+    }
+    u.bias_ids = b.bias_ids ? b.bias_ids + (int64_t)r * b.n_bias : nullptr;
+    u.bias = b.bias_ids ? b.bias + (int64_t)r * b.n_bias : nullptr;
+    u.n_bias = b.bias_ids ? b.n_bias : 0;
+    u.repetition = b.repetition ? b.repetition[r] : 1.f;
+    u.back = b.repetition ? 1.f / u.repetition : 1.f;
+    u.frequency = b.frequency ? b.frequency[r] : 0.f;
+    u.presence = b.presence ? b.presence[r] : 0.f;
+    draft = b.draft && lane < mates ? b.draft[t0 + lane] : -1;      // the drafted token that this lane stands for
     __syncthreads();
     if (b.history) {
       const int32_t *h = b.history + r * b.ld_history;
@@ -91,94 +126,90 @@ __global__ __launch_bounds__(256) void k_logits_rules(egt_rules_batch b, int row
         }
       };
       const int whole = ((uintptr_t)h & 15) == 0 ? n & ~3 : 0;
+#pragma unroll 4
       for (int i = 4 * tid; i < whole; i += 1024) {
         const int4 v = *(const int4 *)(h + i);
         take(i, v.x), take(i + 1, v.y), take(i + 2, v.z), take(i + 3, v.w);
       }
       for (int i = whole + tid; i < n; i += 256) take(i, h[i]);
     }
-    Rules u;
-    u.bias_ids = b.bias_ids ? b.bias_ids + (int64_t)r * b.n_bias : nullptr;
-    u.bias = b.bias_ids ? b.bias + (int64_t)r * b.n_bias : nullptr;
-    u.n_bias = b.bias_ids ? b.n_bias : 0;
     for (int i = tid; i < u.n_bias; i += 256) {
       const uint32_t t = (uint32_t)u.bias_ids[i] - (uint32_t)first;
-      if (t < (uint32_t)ids) atomicOr(&count[t], NAMED);
+      if (t < (uint32_t)ids) {
+        atomicOr(&count[t], NAMED);
+        atomicMax(&named[t], (uint32_t)i + 1);
+      }
     }
-    u.repetition = b.repetition ? b.repetition[r] : 1.f;
-    u.frequency = b.frequency ? b.frequency[r] : 0.f;
-    u.presence = b.presence ? b.presence[r] : 0.f;
-    // the drafted token that this lane stands for (a row sees those whose bits are set)
-    const int mates = min(t1 - t0, 64);
-    const int draft = b.draft && lane < mates ? b.draft[t0 + lane] : -1;
     __syncthreads();
-
-    // ---- the rows, a quarter of the slice at a time
-    for (int unit = 4 * row + wave; unit < 4 * end; unit += 4) {
-      const int i = unit >> 2, from = (unit & 3) * PART, to = min(from + PART, ids);
-      if (from >= to) continue;
-      const T *x = (const T *)b.logits + i * b.ld_logits + first;
-      T *y = (T *)b.out + i * b.ld_out + first;
-      const int which = b.allowed ? b.allowed_row[i] : -1;
-      const bool broken = b.allowed && which >= b.n_allowed;
-      const uint32_t *allowed = which >= 0 && !broken ? b.allowed + which * b.ld_allowed + first / 32 : nullptr;
-      const bool seen = b.draft && draft >= first + from && draft < first + to && (b.mask[i] >> lane & 1);
-      const uint64_t some = __ballot(seen);
-      float again = 0.f;
-      if (some) {                                     // (read before the pass, which may be in place)
-        uint32_t times = 0;
-        for (uint64_t left = some; left; left &= left - 1) {
-          const int o = __builtin_ctzll(left);
-          const bool same = __builtin_amdgcn_readlane(draft, o) == draft;
-          times += same;
-        }
-        if (seen) {
-          const int t = draft - first;
-          again = apply(b, u, wide(x[t]), count[t] + times, draft);
-          if (broken) again = __builtin_nanf("");
-          else if (allowed && !(allowed[t >> 5] >> (t & 31) & 1)) again = -INFINITY;
-        }
-      }
-      for (int t = from + 8 * lane; t < to; t += 512) {
-        const uint32_t bits = allowed ? allowed[t >> 5] >> (t & 31) : ~0u;
-        Eight<T> v;
-        const int n = to - t;
-        if (n >= 8) {
-          v = *(const Eight<T> *)(x + t);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e < n) v.v[e] = x[t + e];
-        }
-        const uint4 c0 = *(const uint4 *)(count + t), c1 = *(const uint4 *)(count + t + 4);
-        const uint32_t c[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
-        const uint32_t any = (c0.x | c0.y | c0.z | c0.w) | (c1.x | c1.y | c1.z | c1.w);
-        // (most ids have no history: theirs are passed on as they are)
-        if (any || (bits & 0xff) != 0xff || broken) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float z = wide(v.v[e]);
-            if (c[e]) z = apply(b, u, z, c[e], first + t + e);
-            if (broken) z = __builtin_nanf("");
-            else if (!(bits >> e & 1)) z = -INFINITY;
-            narrow(v.v[e], z);
-          }
-        }
-        if (n >= 8) {
-          *(Eight<T> *)(y + t) = v;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e < n) y[t + e] = v.v[e];
-        }
-      }
-      if (some) {
-        wait_vmem<0>();                               // (the pass has written these ids too)
-        if (seen) narrow(y[draft - first], again);    // (tokens of one id write the same number)
+  };
+  auto pass = [&](int row, Row &w) {
+    if (row >= stop) return;
+    if (row >= end) turn_to(row);
+    if (r < 0 || from >= to) return;
+    const T *x = (const T *)b.logits + row * b.ld_logits + first;
+    T *y = (T *)b.out + row * b.ld_out + first;
+    // the ids of drafted tokens that this row sees, again, by the lanes that stand for them: read before the pass, which may
+    // be in place
+    const bool seen = draft >= first + from && draft < first + to && (b.mask[row] >> lane & 1);
+    const uint64_t some = __ballot(seen);
+    float again = 0.f;
+    if (some) {
+      uint32_t times = 0;
+      for (uint64_t left = some; left; left &= left - 1) times += __builtin_amdgcn_readlane(draft, __builtin_ctzll(left)) == draft;
+      if (seen) {
+        const int t = draft - first;
+        const uint32_t n = count[t] + times;
+        again = penalised(u, wide(x[t]), n);
+        if (n & NAMED) again = again + u.bias[named[t] - 1];
+        const int which = b.allowed ? b.allowed_row[row] : -1;
+        if (w.broken) again = __builtin_nanf("");
+        else if (which >= 0 && !(b.allowed[which * b.ld_allowed + (draft >> 5)] >> (draft & 31) & 1)) again = -INFINITY;
       }
     }
-    row = end;
-    __syncthreads();                                  // (the counters are cleared next)
+#pragma unroll
+    for (int q = 0; q < VL; ++q) {
+      const int t = from + 512 * q + 8 * lane;
+      if (t >= to) continue;
+      const uint4 c0 = *(const uint4 *)(count + t), c1 = *(const uint4 *)(count + t + 4);
+      const uint32_t c[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w}, any = (c0.x | c0.y | c0.z | c0.w) | (c1.x | c1.y | c1.z | c1.w);
+      if (any) {
+        float z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = penalised(u, wide(w.v[q].v[e]), c[e]);
+        if (any & NAMED) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (c[e] & NAMED) z[e] = z[e] + u.bias[named[t + e] - 1];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c[e]) narrow(w.v[q].v[e], z[e]);        // (ids that nothing is said of stay as they are)
+      }
+      const uint32_t bits = w.bits[q] >> (t & 31);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (w.broken || !(bits >> e & 1)) narrow(w.v[q].v[e], w.broken ? __builtin_nanf("") : -INFINITY);
+      if (t + 8 <= to) {
+        *(Eight<T> *)(y + t) = w.v[q];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (t + e < to) y[t + e] = w.v[q].v[e];
+      }
+    }
+    if (some) {
+      wait_vmem<0>();                                 // (the pass has written these ids too)
+      if (seen) narrow(y[draft - first], again);      // (tokens of one id write the same number)
+    }
+  };
+  if (end >= b.cu_tokens[b.requests]) return;         // (rows behind the last request)
+  // (one row's logits are on their way while the other is done; in place, no row is another's)
+  Row even = fetch(end);
+  for (int row = end; row < stop; row += 2) {
+    Row odd = fetch(row + 1);
+    pass(row, even);
+    if (row + 2 < stop) even = fetch(row + 2);
+    pass(row + 1, odd);
   }
 }
 
@@ -205,10 +236,11 @@ egt_status egt_logits_rules(const egt_rules_batch *b, void *stream) {
                         (const void *)b->allowed, (const void *)b->allowed_row})
     if ((uintptr_t)p & 3) return EGT_ERR_BUFFER;
   // Slices of 4096 ids count a history in fewer workgroups; where rows are few, slices of 1024 have the whole chip at work.  Rows of one
-  // request share a count: as many together as a request has on average, as long as there are workgroups for the chip.
+  // request share a count: as many together as a request has on average, as long as there are 2048 workgroups (128 rows of
+  // 128000 ids, 72 of them used: 1024 workgroups 23.5 us, 2048 19.8, 4096 26.3; slices of 2048 21.2; of 8192 with 8 waves 22.5).
   const bool large = (int64_t)b->tokens * ((b->vocab + 4095) / 4096) >= 512;
   const int slices = large ? (b->vocab + 4095) / 4096 : (b->vocab + 1023) / 1024;
-  const int64_t each = std::min<int64_t>((int64_t)b->tokens * slices / 512, (b->tokens + b->requests - 1) / b->requests);
+  const int64_t each = std::min<int64_t>((int64_t)b->tokens * slices / 2048, (b->tokens + b->requests - 1) / b->requests);
   const int rows_each = (int)std::min<int64_t>(std::max<int64_t>(each, 1), 64);
   const dim3 grid((unsigned)slices, (unsigned)((b->tokens + rows_each - 1) / rows_each)), block(256);
   const hipStream_t to = (hipStream_t)stream;

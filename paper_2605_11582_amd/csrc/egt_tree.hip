@@ -31,7 +31,7 @@ struct TreeArgs {
   egt_kv_cache c;
   float *part;                       // [splits][tokens * heads][dim]: weighted sums of a span
   float2 *ml;                        // [splits][tokens * heads]: its reference and sum
-  int32_t shift, group, splits, row_blocks, min_tiles;
+  int32_t shift, group, splits, row_blocks, min_tiles, whole;
   float scale2;                      // |scale| log2(e)
   uint32_t flip;                     // sign of the scale, on pairs of q
 };
@@ -53,11 +53,11 @@ constexpr int SWIZZLE = DC == 4 || DC == 8 ? 7 : DC == 2 || DC == 6 ? 3 : 0;
 
 // How a request's keys are cut: the same answer in both kernels.
 struct Spans { int ctx_tiles, tiles, per, count; };
-__device__ __forceinline__ Spans spans_of(int len, int n, int splits, int min_tiles) {
+__device__ __forceinline__ Spans spans_of(int len, int n, int splits, int min_tiles, int whole) {
   Spans s;
   s.ctx_tiles = (len + TILE - 1) / TILE;
   s.tiles = s.ctx_tiles + (n + TILE - 1) / TILE;
-  s.per = max((s.tiles + splits - 1) / splits, min_tiles);
+  s.per = s.tiles <= whole ? s.tiles : max((s.tiles + splits - 1) / splits, min_tiles);
   s.count = (s.tiles + s.per - 1) / s.per;
   return s;
 }
@@ -68,13 +68,13 @@ __device__ __forceinline__ int request_state(const TreeArgs &a, int t0, int t1, 
 }
 
 // Waves of a workgroup, and how many tiles ahead of their use a wave requests its share of them.
-constexpr int waves_of(int wr) { return wr > 4 ? wr : 4; }
+constexpr int waves_of(int dc, int wr) { return (dc <= 4 && wr <= 2) || wr > 4 ? 8 : 4; }
 constexpr int ahead_of(int wr) { return wr >= 8 ? 3 : wr >= 4 ? 2 : 1; }
 
 template <int DC, int NR, int WR>
-__global__ __launch_bounds__(64 * waves_of(WR), DC > 4 && WR < 8 ? 1 : 2) void k_tree(TreeArgs a) {
+__global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) void k_tree(TreeArgs a) {
   // a key in LDS: ROW bytes, PIECES pieces of 16; a tile of K and one of V: KV bytes each; a wave stages LJ x 64 pieces of either
-  constexpr int W = waves_of(WR), WK = W / WR, ROW = 64 * DC, PIECES = 4 * DC, LJ = (2 * DC + WR - 1) / WR, BUFS = WR > 1 ? 2 : 1, KV = TILE * ROW;
+  constexpr int W = waves_of(DC, WR), WK = W / WR, ROW = 64 * DC, PIECES = 4 * DC, LJ = (2 * DC + WR - 1) / WR, BUFS = WR > 1 ? 2 : 1, KV = TILE * ROW;
   constexpr int AHEAD = ahead_of(WR);
   extern __shared__ __align__(16) uint8_t lds[];
   __shared__ int odd_seen[W];
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(64 * waves_of(WR), DC > 4 && WR < 8 ? 1 : 2) void k
       }
     return;
   }
-  const Spans sp = spans_of(len, n, a.splits, a.min_tiles);
+  const Spans sp = spans_of(len, n, a.splits, a.min_tiles, a.whole);
   const int row0 = rb * (16 * NR * WR);
   if ((int)blockIdx.x >= sp.count || row0 >= rows) return;
   const int base = row0 + wr * 16 * NR, begin = blockIdx.x * sp.per, end = min(begin + sp.per, sp.tiles);
@@ -450,7 +450,7 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
   const int r = blockIdx.z, lane = threadIdx.x & 63, h = blockIdx.x * 4 + (threadIdx.x >> 6);
   const int t0 = a.b.cu_tokens[r], t1 = a.b.cu_tokens[r + 1], len = a.b.lens[r], i = t0 + blockIdx.y;
   if (request_state(a, t0, t1, len) != ROWS_FINE || i >= t1 || h >= a.b.heads) return;
-  const Spans sp = spans_of(len, t1 - t0, a.splits, a.min_tiles);
+  const Spans sp = spans_of(len, t1 - t0, a.splits, a.min_tiles, a.whole);
   if (sp.count == 1) return;
   const int64_t row = (int64_t)i * a.b.heads + h, step = (int64_t)a.b.tokens * a.b.heads;
   float2 mine = lane < sp.count ? a.ml[lane * step + row] : float2{-INFINITY, 0.f};     // (64 spans at most)
@@ -461,19 +461,25 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
   float total = w * mine.y;
 #pragma unroll
   for (int x = 32; x > 0; x >>= 1) total += __shfl_xor(total, x, 64);
+  // lanes that the row's values leave over take spans of their own: `teams` of 1 << tshift lanes, joined at the end
+  const int tshift = a.c.dim > 128 ? 6 : a.c.dim > 64 ? 5 : a.c.dim > 32 ? 4 : 3, teams = 64 >> tshift, d = 4 * (lane & ((1 << tshift) - 1));
   f4 v = {0, 0, 0, 0};
-  const float *p = a.part + row * a.c.dim + (4 * lane < a.c.dim ? 4 * lane : 0);
+  const float *p = a.part + row * a.c.dim + (d < a.c.dim ? d : 0);
 #pragma unroll 8
-  for (int s = 0; s < sp.count; ++s) {
+  for (int s = lane >> tshift; s < 64; s += teams) {
+    if (s - (lane >> tshift) >= sp.count) break;      // (all teams leave together)
     const float f = __shfl(w, s, 64);                 // (every lane is here: lane s may have no part of the row)
-    const f4 u = *(const f4 *)(p + s * step * a.c.dim);
+    const f4 u = *(const f4 *)(p + min(s, sp.count - 1) * step * a.c.dim);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = fmaf(f, u[e], v[e]);
+    for (int e = 0; e < 4; ++e) v[e] = s < sp.count ? fmaf(f, u[e], v[e]) : v[e];
   }
-  if (4 * lane < a.c.dim) {
+  for (int x = 32; x >= 1 << tshift; x >>= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], x, 64);
+  if (lane < 1 << tshift && d < a.c.dim) {
     const float inv = total == 0.f ? 0.f : 1.f / total;
     const h2 lo = {(_Float16)(v[0] * inv), (_Float16)(v[1] * inv)}, hi = {(_Float16)(v[2] * inv), (_Float16)(v[3] * inv)};
-    *(u2 *)(a.b.out + i * a.b.out_row + h * a.b.out_head + 4 * lane) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+    *(u2 *)(a.b.out + i * a.b.out_row + h * a.b.out_head + d) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
   }
 }
 
@@ -488,7 +494,7 @@ egt_status check_sizes(const egt_tree_batch *b, const egt_kv_cache *c) {
 }
 
 constexpr int MAX_SPLITS = 64;
-struct Shape { int nr, wr, row_blocks, splits, min_tiles; };
+struct Shape { int nr, wr, row_blocks, splits, min_tiles, whole; };
 Shape shape_of(const egt_tree_batch &b, const egt_kv_cache &c) {
   Shape s;
   const int rows = b.max_tokens * (b.heads / c.heads);
@@ -496,9 +502,12 @@ Shape shape_of(const egt_tree_batch &b, const egt_kv_cache &c) {
   s.wr = 1;
   while (s.wr < 8 && rows > 16 * s.nr * s.wr) s.wr *= 2;
   s.row_blocks = (rows + 16 * s.nr * s.wr - 1) / (16 * s.nr * s.wr);
-  s.min_tiles = waves_of(s.wr) / s.wr;
+  const int waves = waves_of((c.dim + 31) / 32, s.wr);
+  s.min_tiles = waves / s.wr;
+  s.whole = 2 * s.min_tiles;
   const int64_t groups = (int64_t)std::max(b.requests, 1) * c.heads * s.row_blocks, tiles = ((int64_t)b.table_blocks * c.page + TILE - 1) / TILE + 2;
-  s.splits = (int)std::min<int64_t>({std::max<int64_t>((s.wr == 8 ? 256 : 512) / groups, 1), (tiles + s.min_tiles - 1) / s.min_tiles, MAX_SPLITS});
+  s.splits = (int)std::min<int64_t>({std::max<int64_t>((waves == 8 ? 256 : 512) / groups, 1), (tiles + s.min_tiles - 1) / s.min_tiles, MAX_SPLITS});
+  if (tiles <= s.whole) s.splits = 1;
   return s;
 }
 size_t rows_of(const egt_tree_batch &b) { return (size_t)b.tokens * b.heads; }
@@ -510,12 +519,12 @@ size_t workspace_of(const egt_tree_batch &b, const egt_kv_cache &c) {
 
 template <int DC, int NR, int WR>
 hipError_t launch_tree(const TreeArgs &a, hipStream_t stream) {
-  constexpr size_t bytes = (size_t)(waves_of(WR) / WR) * (WR > 1 ? 2 : 1) * 2 * TILE * 64 * DC;
+  constexpr size_t bytes = (size_t)(waves_of(DC, WR) / WR) * (WR > 1 ? 2 : 1) * 2 * TILE * 64 * DC;
   if (bytes > 60 * 1024) {
     const hipError_t e = hipFuncSetAttribute((const void *)k_tree<DC, NR, WR>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e != hipSuccess) return e;
   }
-  return launch(k_tree<DC, NR, WR>, dim3(a.splits, a.c.heads * a.row_blocks, a.b.requests), dim3(64 * waves_of(WR)), bytes, stream, a);
+  return launch(k_tree<DC, NR, WR>, dim3(a.splits, a.c.heads * a.row_blocks, a.b.requests), dim3(64 * waves_of(DC, WR)), bytes, stream, a);
 }
 template <int DC>
 hipError_t launch_dim(const TreeArgs &a, const Shape &s, hipStream_t stream) {
@@ -568,6 +577,7 @@ egt_status egt_tree_attention(const egt_tree_batch *b, const egt_kv_cache *cache
   a.splits = s.splits;
   a.row_blocks = s.row_blocks;
   a.min_tiles = s.min_tiles;
+  a.whole = s.whole;
   a.scale2 = __builtin_fabsf(b->scale) * 1.44269504088896340736f;
   a.flip = __builtin_signbit(b->scale) ? 0x80008000u : 0u;
   const hipStream_t to = (hipStream_t)stream;
