@@ -244,18 +244,41 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
   auto compute = [&](int i) {
       const int t = tile_of(i), limit = limit_of(i);
       const bool drafted = t >= sp.ctx_tiles;
+      // Reads ahead of the products that use them, and kept there: left alone, the compiler waits for them two by two (a step of
+      // two row tiles: scores 650 cycles and weighted sums 940, of 256 and 288 that the products take).
       f4 s[NR][2];
-#pragma unroll
-      for (int x = 0; x < NR; ++x) s[x][0] = s[x][1] = f4{0, 0, 0, 0};
+      u4 k[2][DC];
 #pragma unroll
       for (int c = 0; c < DC; ++c)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int key = 16 * h + n16;
-          const h8 k = __builtin_bit_cast(h8, *(const u4 *)(k_area(i) + key * ROW + 32 * ((2 * c + (g4 >> 1)) ^ turn(key)) + 16 * (g4 & 1)));
-#pragma unroll
-          for (int x = 0; x < NR; ++x) s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[x][c], s[x][h], 0, 0, 0);
+          k[h][c] = *(const u4 *)(k_area(i) + key * ROW + 32 * ((2 * c + (g4 >> 1)) ^ turn(key)) + 16 * (g4 & 1));
         }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < NR; ++x) s[x][0] = s[x][1] = f4{0, 0, 0, 0};
+#pragma unroll
+      for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int x = 0; x < NR; ++x)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, k[h][c]), q[x][c], s[x][h], 0, 0, 0);
+      // V^T as the A operand: lane j of a group of 16 addresses 8 bytes of key 4 g + j / 4, and gets d = 16 dt + n of keys 4 g .. 4 g + 3
+      constexpr int FAR = 4;
+      u4 v[FAR];
+      auto read_v = [&](int d) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int key = 16 * h + 4 * g4 + (n16 >> 2);
+          const u2 both = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(v_area(i) + key * ROW + 32 * (d ^ turn(key)) + 8 * (n16 & 3))));
+          v[d % FAR][2 * h] = both.x;
+          v[d % FAR][2 * h + 1] = both.y;
+        }
+      };
+#pragma unroll
+      for (int d = 0; d < FAR; ++d) read_v(d);
+      __builtin_amdgcn_sched_barrier(0);
       if (drafted || limit < TILE) {
 #pragma unroll
         for (int x = 0; x < NR; ++x) {
@@ -309,19 +332,13 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
         for (int j = 0; j < 8; ++j) p[x][j] = (_Float16)e[x][j];
 #pragma unroll
       for (int x = 0; x < NR; ++x) l[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p[x], l[x], 0, 0, 0);      // (every entry of a row: its sum)
-      // V^T as the A operand: lane j of a group of 16 addresses 8 bytes of key 4 g + j / 4, and gets d = 16 dt + n of keys 4 g .. 4 g + 3
 #pragma unroll
       for (int d = 0; d < 2 * DC; ++d) {
-        u4 v;
+        const u4 now = v[d % FAR];
+        if (d + FAR < 2 * DC) read_v(d + FAR);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int key = 16 * h + 4 * g4 + (n16 >> 2);
-          const u2 both = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(v_area(i) + key * ROW + 32 * (d ^ turn(key)) + 8 * (n16 & 3))));
-          v[2 * h] = both.x;
-          v[2 * h + 1] = both.y;
-        }
-#pragma unroll
-        for (int x = 0; x < NR; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, v), p[x], o[x][d], 0, 0, 0);
+        for (int x = 0; x < NR; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, now), p[x], o[x][d], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
   };
 #pragma unroll 1
