@@ -494,7 +494,8 @@ egt_status egt_kv_append(const egt_append_batch *b, const egt_kv_cache *cache, v
  * FP16 in and out; scores, maxima, sums and the weighted sum in FP32, the weights rounded to
  * FP16 for the matrix cores (relative to the largest, down to 2^-24 of it).
  * dim: a multiple of 8 up to 256; pointers and strides whole 16 bytes; k and v have the cache's heads;
- * the pages of the cache, and the tokens of a page, lie less than 2^31 elements apart.  `out` must not overlap an input.
+ * rows, pages and tokens of a page lie less than 2^31 elements apart; heads <= 4096, requests <= EGT_MAX_REQUESTS,
+ * table_blocks * page at most 2^30.  `out` must not overlap an input.
  * egt_tree_attention_ws_bytes (HOST): bytes of workspace (DEVICE, 16-byte aligned) that a call
  * of these requests, tokens, heads, max_tokens, table_blocks and cache sizes needs, never less
  * than 16; the pointers are not looked at.  The workspace is dead after the call's kernels; calls that share one must not overlap.

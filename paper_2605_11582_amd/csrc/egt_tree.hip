@@ -84,15 +84,16 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
   const int t0 = a.b.cu_tokens[r], t1 = a.b.cu_tokens[r + 1], len = a.b.lens[r];
   const int state = request_state(a, t0, t1, len);
   if (state == ROWS_NONE) return;
-  const int n = t1 - t0, rows = n * a.group;
-  if (state == ROWS_BAD) {
+  const int n = t1 - t0;
+  if (state == ROWS_BAD) {                            // (any number of tokens)
     if (blockIdx.x == 0 && rb == 0)
-      for (int64_t e = threadIdx.x; e < (int64_t)rows * dim; e += 64 * W) {
-        const int row = (int)(e / dim), d = (int)(e % dim);
-        a.b.out[(int64_t)(t0 + row / a.group) * a.b.out_row + (int64_t)(kh * a.group + row % a.group) * a.b.out_head + d] = 0x7e00;
+      for (int64_t e = threadIdx.x; e < (int64_t)n * a.group * dim; e += 64 * W) {
+        const int64_t row = e / dim, tok = row / a.group;
+        a.b.out[(t0 + tok) * a.b.out_row + (kh * a.group + row - tok * a.group) * a.b.out_head + e - row * dim] = 0x7e00;
       }
     return;
   }
+  const int rows = n * a.group;
   const Spans sp = spans_of(len, n, a.splits, a.min_tiles, a.whole);
   const int row0 = rb * (16 * NR * WR);
   if ((int)blockIdx.x >= sp.count || row0 >= rows) return;
@@ -505,7 +506,7 @@ egt_status check_sizes(const egt_tree_batch *b, const egt_kv_cache *c) {
   const egt_status st = check_cache(c, false);
   if (st != EGT_OK) return st;
   if (b->requests < 0 || b->tokens < 0 || b->heads < 1 || b->heads % c->heads != 0 || b->max_tokens < 1 || b->max_tokens > EGT_MAX_TREE || b->table_blocks < 0 ||
-      (int64_t)b->table_blocks * c->page >= (1ll << 31))
+      (int64_t)b->table_blocks * c->page > (1ll << 30))
     return EGT_ERR_SHAPE;
   return b->requests > EGT_MAX_REQUESTS || b->heads > 4096 ? EGT_ERR_UNSUPPORTED : EGT_OK;
 }
