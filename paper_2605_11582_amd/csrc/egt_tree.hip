@@ -520,8 +520,10 @@ Shape shape_of(const egt_tree_batch &b, const egt_kv_cache &c) {
   s.wr = 1;
   while (s.wr < 8 && rows > 16 * s.nr * s.wr) s.wr *= 2;
   s.row_blocks = (rows + 16 * s.nr * s.wr - 1) / (16 * s.nr * s.wr);
+  // A span is a tile a wave at least, and four tiles; up to two tiles a wave, and eight tiles, stay whole, for joining costs a launch (us,
+  // one token over 777 keys of 32 heads: four spans and a join 13.7, one span of 3.4 tiles a wave 15.2; over 300 keys: three spans 12.8, one 11.8).
   const int waves = waves_of((c.dim + 31) / 32, s.wr);
-  s.min_tiles = waves / s.wr;
+  s.min_tiles = std::max(waves / s.wr, 4);
   s.whole = 2 * s.min_tiles;
   const int64_t groups = (int64_t)std::max(b.requests, 1) * c.heads * s.row_blocks, tiles = ((int64_t)b.table_blocks * c.page + TILE - 1) / TILE + 2;
   s.splits = (int)std::min<int64_t>({std::max<int64_t>((waves == 8 ? 256 : 512) / groups, 1), (tiles + s.min_tiles - 1) / s.min_tiles, MAX_SPLITS});
