@@ -758,7 +758,8 @@ def prepared_gemm_stack(items, stream=None):
 # ------------------------------------------------- beside the products of a verification step
 # egt.h says what each of them computes.  Tensors are checked and marshalled in the extension module (a ValueError names
 # the argument that is wrong); they are all on one device, and without `stream` the call goes to that device's current
-# stream.  The prepared forms marshal once and launch on every call; they keep the tensors alive.
+# stream.  The prepared forms marshal once and launch on every call, with the tensors' device as the current one; they keep the
+# tensors alive.
 def kv_slots(lens, counts, block_table, page: int, blocks: int, free_blocks, free_head, slots, cu_tokens, new_lens, new_head, stream=None) -> None:
     """Block tables and slot maps of requests that grow from lens by counts tokens: int32 device tensors
     lens, counts, new_lens (R,), block_table (R, W), free_blocks (F,), free_head, new_head (1,), slots (N,),

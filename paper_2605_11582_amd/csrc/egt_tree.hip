@@ -1,18 +1,24 @@
 // Attention of drafted trees over a paged cache.
 //
 // Of one request and one key head, all query rows - its drafted tokens times the query heads that share the key head - meet
-// the same keys: the cache is read once for all of them.  A workgroup has four waves, WR of them side by side over the rows
-// (16 NR rows each) and 4 / WR over the keys; a wave takes 32 keys at a time, and the grid cuts the keys into `splits` spans
-// where requests and heads alone do not fill the chip.  Nothing in the loop is shared between waves, so there is no barrier in it:
+// the same keys: the cache is read once for all of them.  A workgroup has W waves, WR of them side by side over the rows
+// (16 NR rows each) and W / WR groups of them over the keys; a group takes 32 keys at a time, and the grid cuts the keys into spans
+// where requests and heads alone do not fill the chip (a second kernel joins them).  A step of a group:
 //
-//   S^T = K Q^T    K straight from the cache into the A operand (a lane: one key, 8 values of d), Q^T held in registers.
-//                  Lane (g, n) gets scores of row n and keys 4 g .. 4 g + 3 of either half of the 32.
+//   stage          K and V of 32 keys through registers into LDS, each wave its share, in whole lines of the cache; the tiles
+//                  behind them are on their way.  Groups of several waves have two buffers and meet in one barrier a step.
+//   S^T = K Q^T    a lane: one key, 8 values of d; Q^T is held in registers.  Lane (g, n) gets scores of row n and keys
+//                  4 g .. 4 g + 3 of either half of the 32.
 //   p = exp2       against a reference per row that is raised only where a score passes it by 2^5: sums and O are rescaled
 //                  rarely, and the maximum is joined over lanes only then.
-//   O^T += V^T P^T the scores' layout is the B operand's if the 32 keys are counted 4 g + i, 16 + 4 g + i, so p goes on in its lane; V^T comes
-//                  out of LDS (a wave's own 32 keys) by the transposing read.
+//   O^T += V^T P^T the scores' layout is the B operand's if the 32 keys are counted 4 g + i, 16 + 4 g + i, so p goes on in its lane;
+//                  V^T comes out of LDS by the transposing read; the sum of p is one more product, with ones.
 //
-// What bounds it: the cache's bytes while a key head has up to about 128 rows; above that matrix and exponential work.
+// What bounds it: with up to 64 rows a key head the cache's bytes (16 rows over 131072 keys, 8 heads of 128: 107 us, 5.0 TB/s;
+// 64 rows 116 us), above that the steps themselves, of which one wave a SIMD can hide little: 256 rows 187 us, 2.9 TB/s and
+// 0.73 PFLOP/s, matrix units busy 38 % of the time and vector units 46 %.  A wave of two row tiles spends, of 2500 cycles a step,
+// 345 on staging, 500 on addresses and requests, 610 on scores (256 of them products), 390 on weights and 555 on sums (288).  Short
+// contexts are bound by a launch and the chain lengths - page numbers - keys, 9 us, and a launch more where there are several spans.
 #include "egt_mfma_common.h"
 #include "egt_serve.h"
 
@@ -40,7 +46,7 @@ typedef __attribute__((address_space(1))) u4 global_u4;
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s4v lds_s4v;
 
-// 1 in the halves of a pair that are infinite or NaN, as whole-half masks
+// All ones in the halves of a pair that are infinite or NaN.
 __device__ __forceinline__ uint32_t odd_halves(uint32_t x) {
   const uint32_t lo = (x & 0x7c00u) == 0x7c00u ? 0xffffu : 0u, hi = (x & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u;
   return lo | hi;
@@ -67,7 +73,9 @@ __device__ __forceinline__ int request_state(const TreeArgs &a, int t0, int t1, 
   return t1 - t0 > a.b.max_tokens || len < 0 || len > (int64_t)a.b.table_blocks << a.shift || (len > 0 && a.c.blocks == 0) ? ROWS_BAD : ROWS_FINE;
 }
 
-// Waves of a workgroup, and how many tiles ahead of their use a wave requests its share of them.
+// Waves of a workgroup, and how many tiles ahead of their use a wave requests its share of them.  Eight waves where few rows leave most
+// of them to the keys (us, eight against four: one token over 8000 keys of 8 heads 21.5 / 34.7, 32 requests over up to 2000 31.9 / 35.5),
+// four where barriers tie them together; wide heads have no LDS for eight groups.
 constexpr int waves_of(int dc, int wr) { return (dc <= 4 && wr <= 2) || wr > 4 ? 8 : 4; }
 constexpr int ahead_of(int wr) { return wr >= 8 ? 3 : wr >= 4 ? 2 : 1; }
 
@@ -516,6 +524,8 @@ struct Shape { int nr, wr, row_blocks, splits, min_tiles, whole; };
 Shape shape_of(const egt_tree_batch &b, const egt_kv_cache &c) {
   Shape s;
   const int rows = b.max_tokens * (b.heads / c.heads);
+  // Two row tiles a wave from 65 rows on (up to 128 rows, us, two tiles of four waves against one of eight: sixteen requests of up to 80 rows
+  // 52.8 / 53.9, 128 rows over 131072 keys 151 / 185); wider heads have no registers for them.
   s.nr = rows <= 64 || c.dim > 128 ? 1 : 2;
   s.wr = 1;
   while (s.wr < 8 && rows > 16 * s.nr * s.wr) s.wr *= 2;

@@ -679,3 +679,77 @@ def test_empty_batches():
     egt.logits_rules(z(0, 100), z(0, 100), i(1))
     egt.logits_rules(z(3, 0), z(3, 0), i(2))
     torch.cuda.synchronize()
+
+
+def test_an_error_of_the_hip_runtime_is_raised_by_the_call_that_meets_it():
+    """Entry points that fail with a HIP error: one call, one exception, plain and prepared."""
+    import ctypes as C
+    rng = np.random.default_rng(60)
+    calls = []
+    types = {"egt_kv_slots": 2, "egt_kv_append": 3, "egt_tree_attention": 5, "egt_tree_attention_ws_bytes": 3, "egt_lora_smallm": 4, "egt_logits_rules": 2}
+
+    def failing(name):
+        def entry(*a):
+            calls.append(name)
+            return 7
+        return C.CFUNCTYPE(C.c_int, *[C.c_size_t if (name, k) in (("egt_tree_attention", 3), ("egt_lora_smallm", 2)) else C.c_void_p for k in range(types[name])])(entry)
+    c = tree_case(rng, [20], [3], 4, 2, 64, 16)
+    a = lora_case(rng, 4, 64, 40, 8, 2)
+    i = dev(np.zeros(4, np.int32))
+    fns = [failing(name) for name in egt._batches]
+    native = egt._native()
+    native.bind_batches(*[C.cast(f, C.c_void_p).value for f in fns])
+    tree = (c["q"], c["k"], c["v"], c["k_cache"], c["v_cache"], dev(c["table"]), dev(c["lens"]), dev(c["cu"]), dev(c["mask"]), c["out"], 1.0, 3, c["ws"])
+    slots = (i[:2], i[:2], i.view(2, 2), 16, 4, i, i[:1], i, i[:3], i[:2], i[:1])
+    try:
+        for name, args in (("kv_slots", slots), ("kv_append", (c["k"], c["v"], dev(np.zeros(5, np.int32)), c["k_cache"], c["v_cache"])), ("tree_attention", tree),
+                           ("lora_smallm", (a["X"], a["A"], a["B"], dev(a["index"]), a["Y"], a["ws"])), ("logits_rules", (a["Y"], a["Y"], dev(np.array([0, 4], np.int32))))):
+            for call in (lambda: getattr(egt, name)(*args), lambda: getattr(egt, "prepared_" + name)(*args)()):
+                with pytest.raises(egt.EgtError) as e:
+                    call()
+                assert e.value.status == 7 and calls == ["egt_" + name]
+                calls.clear()
+    finally:
+        egt._call = None
+        egt._native()
+    run_tree(c)
+
+
+def test_refused_calls_write_nothing():
+    torch = G.torch_mod()
+    rng = np.random.default_rng(61)
+    a = lora_case(rng, 4, 64, 40, 8, 2)
+    call = lambda **k: egt.lora_smallm(**{**dict(X=a["X"], A=a["A"], B=a["B"], index=dev(a["index"]), Y=a["Y"], workspace=a["ws"], base=a["base"], scale=dev(a["scale"])), **k})  # noqa: E731
+    a["wide"].fill_(9.0)
+    for wrong in (dict(X=a["X"][:, :56]), dict(A=a["A"].float()), dict(B=a["B"][:1]), dict(B=a["B"].transpose(0, 1)), dict(index=dev(np.zeros(3, np.int32))), dict(Y=a["Y"][:3]),
+                  dict(base=a["base"][:, :39]), dict(scale=dev(np.ones(3, np.float32))), dict(Y=a["Y"][:1].expand(4, -1)), dict(workspace=a["ws"].cpu())):
+        with pytest.raises(ValueError):
+            call(**wrong)
+    for wrong, status in ((dict(workspace=None), 1), (dict(workspace=a["ws"][:4]), 2), (dict(X=a["X"].repeat(17, 1), Y=a["Y"].repeat(17, 1), base=None, index=dev(np.zeros(68, np.int32))), 2)):
+        with pytest.raises(egt.EgtError) as e:
+            call(**wrong)
+        assert e.value.status == status
+    r, logits, buf, out = rules_case(rng, [3, 1], 1000, 20, "fp16")
+    rules = lambda **k: egt.logits_rules(**{**dict(logits=logits, out=out, cu_tokens=dev(r["cu"]), history=dev(r["history"]), history_len=dev(r["history_len"])), **k})  # noqa: E731
+    for wrong in (dict(out=out.float()), dict(out=out[:, :999]), dict(history_len=None), dict(history=dev(r["history"][:1])), dict(draft=dev(r["draft"])), dict(mask=dev(r["mask"])),
+                  dict(allowed=dev(r["allowed"])), dict(allowed=dev(r["allowed"])[:, :31], allowed_row=dev(r["allowed_row"])), dict(bias_ids=dev(r["bias_ids"])), dict(repetition=dev(r["repetition"])[:1]),
+                  dict(logits=logits.bfloat16()), dict(out=out.t()), dict(cu_tokens=dev(r["cu"])[:0])):
+        with pytest.raises(ValueError):
+            rules(**wrong)
+    k = dev(f16(rng, 4, 2, 64))
+    cache = dev(f16(rng, 3, 2, 16, 64))
+    append = lambda **o: egt.kv_append(**{**dict(k=k, v=k, slots=dev(np.zeros(4, np.int32)), k_cache=cache, v_cache=cache), **o})  # noqa: E731
+    before = cache.clone()
+    for wrong in (dict(slots=dev(np.zeros(3, np.int32))), dict(v=k[:3]), dict(k=k[:, :1]), dict(k_cache=cache[:, :, :, :56]), dict(v_cache=cache[:2]), dict(k_cache=cache[:1].expand(3, -1, -1, -1)),
+                  dict(rows=dev(np.zeros(3, np.int32))), dict(slots=dev(np.zeros(4, np.int64)))):
+        with pytest.raises(ValueError):
+            append(**wrong)
+    with pytest.raises(egt.EgtError) as e:                # (a page of 12 tokens)
+        append(k_cache=cache[:, :, :12], v_cache=cache[:, :, :12])
+    assert e.value.status == 2
+    i = dev(np.zeros(8, np.int32))
+    for wrong in (dict(counts=i[:3]), dict(block_table=i.view(4, 2)), dict(cu_tokens=i[:2]), dict(new_head=i[:2]), dict(page=16.0), dict(slots=i.long()), dict(block_table=i[:2].view(2, 1).expand(2, 3))):
+        with pytest.raises(ValueError):
+            egt.kv_slots(**{**dict(lens=i[:2], counts=i[2:4], block_table=i.view(2, 4), page=16, blocks=4, free_blocks=i, free_head=i[:1], slots=i, cu_tokens=i[:3], new_lens=i[4:6], new_head=i[7:]), **wrong})
+    torch.cuda.synchronize()
+    assert (a["wide"] == 9).all() and (out == 5).all() and torch.equal(cache, before)
