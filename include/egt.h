@@ -471,7 +471,7 @@ egt_status egt_kv_slots(const egt_slots_batch *b, void *stream);
  * row i) of k and v goes to slot slots[i], for i < n.  Entries whose slot is not one of the
  * cache's (-1: rejected, padding) or whose row is not one of the n_rows are passed over.  Element d of head h of
  * row i is at k[i * k_row + h * k_head + d]; strides as in the cache.  The slots of a call are
- * meant to be different; where two are the same, each 16 bytes are one of the two rows'. */
+ * meant to be different; where two are the same, each 16 bytes are one of the two rows'.  n < 2^24. */
 typedef struct {
   const uint16_t *k, *v;
   const int32_t *slots, *rows;        /* [n]; rows may be NULL                               */
@@ -495,7 +495,7 @@ egt_status egt_kv_append(const egt_append_batch *b, const egt_kv_cache *cache, v
  * FP16 for the matrix cores (relative to the largest, down to 2^-24 of it).
  * dim: a multiple of 8 up to 256; pointers and strides whole 16 bytes; k and v have the cache's heads;
  * rows, pages and tokens of a page lie less than 2^31 elements apart; heads <= 4096, requests <= EGT_MAX_REQUESTS,
- * table_blocks * page at most 2^30.  `out` must not overlap an input.
+ * table_blocks * page at most 2^30, |scale| at most 2^126 (no NaN).  `out` must not overlap an input.
  * egt_tree_attention_ws_bytes (HOST): bytes of workspace (DEVICE, 16-byte aligned) that a call
  * of these requests, tokens, heads, max_tokens, table_blocks and cache sizes needs, never less
  * than 16; the pointers are not looked at.  The workspace is dead after the call's kernels; calls that share one must not overlap.
@@ -526,7 +526,8 @@ egt_status egt_tree_attention(const egt_tree_batch *b, const egt_kv_cache *cache
  * per adapter, NULL for ones.  index[m] < 0: no adapter, Y[m] = base[m]; index[m] >= adapters:
  * NaN.  Any token may have any adapter, and tokens of one adapter read it once.
  * FP32 sums in a fixed order; A . X[m] goes on as two FP16 numbers that hold 22 of its bits.
- * cols and rank multiples of 8, rank <= 128, adapters >= 1; X, A, B, a_stride, b_stride and ldx whole 16 bytes.
+ * What is not finite in an adapter gives infinities or NaN in its own tokens alone.
+ * cols and rank multiples of 8, rank <= 128, cols and rows <= 2^30, adapters >= 1; X, A, B, a_stride, b_stride and ldx whole 16 bytes.
  * Workspace as for egt_tree_attention; egt_lora_smallm_ws_bytes is the HOST query. */
 typedef struct {
   const uint16_t *X, *A, *B, *base;
@@ -543,6 +544,7 @@ egt_status egt_lora_smallm(const egt_lora_batch *b, void *workspace, size_t work
  * logits.  For row i of request r and token id t, in this order and in FP32, rounded once:
  *   x = logits[i][t]
  *   t written or in the prompt:  x = x > 0 ? x / repetition[r] : x * repetition[r]
+ *                                (the quotient as a product with 1 / repetition[r])
  *   t written c > 0 times:       x = x - frequency[r] * c;  x = x - presence[r]
  *   t in bias_ids[r]:            x = x + bias[r] of its last entry
  *   t not allowed:               x = -infinity
@@ -556,7 +558,8 @@ egt_status egt_lora_smallm(const egt_lora_batch *b, void *workspace, size_t work
  * (with bias) and allowed (with allowed_row) may be NULL: that rule is left out, and a prompt_len of NULL is no prompt.
  * kind: EGT_LOGITS_FP16 or EGT_LOGITS_FP32, of logits and out.  out may be logits itself (same
  * leading dimension) and must not overlap it otherwise.  Up to 64 tokens a request see each other: bits past a
- * request's tokens are passed over.  requests <= EGT_MAX_REQUESTS. */
+ * request's tokens are passed over.  requests <= EGT_MAX_REQUESTS, tokens <= 65535, vocab <= 2^30,
+ * history_width and n_bias <= 2^29. */
 enum { EGT_LOGITS_FP16 = 0, EGT_LOGITS_FP32 = 1 };
 typedef struct {
   const void *logits;

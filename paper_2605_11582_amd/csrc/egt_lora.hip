@@ -224,7 +224,7 @@ hipError_t launch_expand(const egt_lora_batch &b, const float *part, int slices,
 
 egt_status check_sizes(int M, int cols, int rank) {
   if (M < 1 || M > 64 || cols < 8 || cols % 8 != 0 || rank < 8 || rank % 8 != 0) return EGT_ERR_SHAPE;
-  return rank > MAX_RANK ? EGT_ERR_UNSUPPORTED : EGT_OK;
+  return rank > MAX_RANK || cols > 1 << 30 ? EGT_ERR_UNSUPPORTED : EGT_OK;
 }
 int slices_of(int cols) { return (cols + SLICE - 1) / SLICE; }
 size_t workspace_of(int M, int cols, int rank) { return 4 * (size_t)slices_of(cols) * M * rank; }
@@ -248,6 +248,7 @@ egt_status egt_lora_smallm(const egt_lora_batch *b, void *workspace, size_t work
   if (b->rows < 0 || b->adapters < 1 || b->ldx < b->cols || b->ldy < b->rows || (b->base && b->ldbase < b->rows) ||
       (b->base == b->Y && b->base && b->ldbase != b->ldy) || b->a_stride < 0 || b->b_stride < 0)
     return EGT_ERR_SHAPE;
+  if (b->rows > 1 << 30) return EGT_ERR_UNSUPPORTED;
   if (b->rows == 0) return EGT_OK;                    // nothing to compute, pointers not examined
   if (!b->X || !b->A || !b->B || !b->Y || !b->index || !workspace) return EGT_ERR_NULL;
   if (workspace_bytes < egt::workspace_of(b->M, b->cols, b->rank)) return EGT_ERR_SHAPE;

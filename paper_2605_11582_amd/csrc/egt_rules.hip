@@ -224,7 +224,7 @@ egt_status egt_logits_rules(const egt_rules_batch *b, void *stream) {
       b->ld_logits < b->vocab || b->ld_out < b->vocab || b->history_width < 0 || (b->history && b->ld_history < b->history_width) || b->ld_allowed < 0 || (b->allowed && b->ld_allowed < ((int64_t)b->vocab + 31) / 32) ||
       (b->logits == b->out && b->ld_logits != b->ld_out))
     return EGT_ERR_SHAPE;
-  if (b->requests > EGT_MAX_REQUESTS || b->tokens > 65535 || b->vocab > (1 << 30)) return EGT_ERR_UNSUPPORTED;
+  if (b->requests > EGT_MAX_REQUESTS || b->tokens > 65535 || b->vocab > (1 << 30) || b->history_width > (1 << 29) || b->n_bias > (1 << 29)) return EGT_ERR_UNSUPPORTED;
   if (b->requests == 0 || b->tokens == 0 || b->vocab == 0) return EGT_OK;
   if (!b->logits || !b->out || !b->cu_tokens || (b->history && !b->history_len) || (b->draft && !b->mask) || (b->bias_ids && !b->bias) ||
       (b->allowed && !b->allowed_row))

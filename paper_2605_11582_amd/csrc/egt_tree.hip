@@ -587,7 +587,7 @@ egt_status egt_tree_attention(const egt_tree_batch *b, const egt_kv_cache *cache
   if (st != EGT_OK) return st;
   st = egt::check_cache(cache, true);
   if (st != EGT_OK) return st;
-  if (b->ld_table < b->table_blocks || !(b->scale == b->scale)) return EGT_ERR_SHAPE;
+  if (b->ld_table < b->table_blocks || !(__builtin_fabsf(b->scale) <= 0x1p126f)) return EGT_ERR_SHAPE;
   if (std::max({cache->k_block, cache->v_block, cache->k_token, cache->v_token, b->k_row, b->v_row}) >= 1ll << 31) return EGT_ERR_UNSUPPORTED;
   if (b->requests == 0 || b->tokens == 0) return EGT_OK;
   if (!b->q || !b->k || !b->v || !b->out || !b->lens || !b->cu_tokens || !b->mask || (b->table_blocks && !b->block_table) || !workspace) return EGT_ERR_NULL;
@@ -608,7 +608,7 @@ egt_status egt_tree_attention(const egt_tree_batch *b, const egt_kv_cache *cache
   a.row_blocks = s.row_blocks;
   a.min_tiles = s.min_tiles;
   a.whole = s.whole;
-  a.scale2 = __builtin_fabsf(b->scale) * 1.44269504088896340736f;
+  a.scale2 = std::max(__builtin_fabsf(b->scale) * 1.44269504088896340736f, 0x1p-126f);      // (zero times a masked score would be NaN)
   a.flip = __builtin_signbit(b->scale) ? 0x80008000u : 0u;
   const hipStream_t to = (hipStream_t)stream;
   hipError_t e;

@@ -193,6 +193,15 @@ def test_attention_of_large_scores():
     check_tree(tree_case(np.random.default_rng(5), [300, 20], [9, 40], 8, 2, 128, 16, scale=6.0))
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-40, -0.125, -3.0])
+def test_attention_of_other_scales(scale):
+    """Every visible key weighs the same where the scale is zero, and what is masked still does not enter."""
+    c = tree_case(np.random.default_rng(30), [0, 45, 300], [7, 40, 3], 4, 2, 64, 16)
+    c["scale"] = scale
+    c["mask"][3] = 0
+    check_tree(c, scale)
+
+
 def test_attention_rows_that_see_nothing_and_other_masks():
     rng = np.random.default_rng(6)
     c = tree_case(rng, [0, 70, 0], [40, 20, 64], 6, 2, 64, 16)

@@ -173,6 +173,74 @@ def test_tensors_without_memory_are_refused():
         torch.vmap(body)(torch.empty((3, 4, 8, 64), dtype=torch.float16, device="cuda"), torch.empty((3, 4), dtype=torch.int32, device="cuda"))
 
 
+LAUNCHES = r"""
+import ctypes as C, itertools, sys
+sys.path.insert(0, {root!r})
+sys.path.insert(0, {root!r} + "/tests")
+from paper_2605_11582_amd import binding as B
+L, P = B._declare(C.CDLL(B.LIB_PATH)), 1 << 20             # (without PyTorch)
+need = C.c_size_t()
+for dim, kv, group, most, requests, table, page in itertools.product((8, 64, 72, 96, 128, 160, 192, 200, 256), (1, 8), (1, 3, 16), (1, 7, 64), (1, 40, 8192), (0, 3, 4096), (1, 16)):
+    heads = kv * group
+    c = B.KvCache(k=P, v=P, blocks=8, heads=kv, page=page, dim=dim, k_block=8, k_head=8, k_token=8, v_block=8, v_head=8, v_token=8)
+    b = B.TreeBatch(q=P, k=P, v=P, out=P, q_row=8, q_head=8, k_row=8, k_head=8, v_row=8, v_head=8, out_row=8, out_head=8, block_table=P, lens=P, cu_tokens=P, mask=P,
+                    ld_table=table, requests=requests, tokens=requests * most, heads=heads, max_tokens=most, table_blocks=table, scale=1.0)
+    assert L.egt_tree_attention_ws_bytes(C.byref(b), C.byref(c), C.byref(need)) == 0
+    print("case", dim, kv, group, most, requests, table, page, need.value, flush=True)
+    assert L.egt_tree_attention(C.byref(b), C.byref(c), P, need.value, None) == 0
+"""
+
+
+def test_launches_of_tree_attention(tmp_path):
+    """Every shape has a kernel, with LDS that a compute unit has, a grid that the runtime takes, and partial results that fit the workspace
+    (a stand-in for the runtime's launch writes down what would run)."""
+    import test_kernel_routes as routes
+    cc = shutil.which("gcc")
+    if not cc:
+        pytest.skip("no host compiler")
+    lib = str(tmp_path / "launch.so")
+    (tmp_path / "launch.c").write_text(routes.STAND_IN.replace('printf("launch %s %u %u %u %zu\\n", name, grid.x, grid.y, block.x, lds);',
+                                                               'printf("launch %s %u %u %u %u %zu\\n", name, grid.x, grid.y, grid.z, block.x, lds);'))
+    subprocess.run([cc, "-shared", "-fPIC", "-O1", str(tmp_path / "launch.c"), "-o", lib], check=True)
+    env = dict(os.environ)
+    env["LD_PRELOAD"] = " ".join(v for v in (lib, env.get("LD_PRELOAD", "")) if v)
+    out = subprocess.run([os.sys.executable, "-c", LAUNCHES.replace("{root!r}", repr(ROOT))], capture_output=True, text=True, env=env, timeout=300)
+    assert out.returncode == 0, (out.stdout[-300:], out.stderr[-2000:])
+    case, kernels = None, set()
+    for line in out.stdout.splitlines():
+        word = line.split()
+        if word[0] == "case":
+            dim, kv, group, most, requests, table, page, need = (int(w) for w in word[1:])
+            case, launches = line, []
+            continue
+        x, y, z, threads, lds = (int(w) for w in word[2:])
+        launches.append(word[1])
+        assert 1 <= x and 1 <= y <= 65535 and 1 <= z <= 65535 and x * threads < 1 << 32 and threads <= 1024 and lds <= 158 * 1024, (case, line)
+        if "k_tree_join" in word[1]:
+            splits = first[0]
+            assert len(launches) == 2 and 1 < splits <= 64 and need >= 4 * splits * requests * most * kv * group * (dim + 2), (case, line)
+        else:
+            first = (x, y, z)
+            kernels.add(word[1])
+            assert len(launches) == 1 and z == requests and y % kv == 0, (case, line)
+    assert len(kernels) >= 20
+
+
+BIG = 1 << 30
+
+
+@pytest.mark.parametrize("status,call", [
+    (UNSUPPORTED, lambda L: L.egt_kv_append(C.byref(append(n=1 << 24)), C.byref(cache()), None)),
+    (SHAPE, lambda L: L.egt_tree_attention(C.byref(tree(scale=float("inf"))), C.byref(cache()), P, BIG, None)),
+    (SHAPE, lambda L: L.egt_tree_attention(C.byref(tree(scale=-2.0 ** 127)), C.byref(cache()), P, BIG, None)),
+    (UNSUPPORTED, lambda L: L.egt_lora_smallm(C.byref(lora(rows=BIG + 1, ldy=BIG + 1, ldbase=BIG + 1)), P, BIG, None)),
+    (UNSUPPORTED, lambda L: L.egt_lora_smallm(C.byref(lora(cols=BIG + 8, ldx=BIG + 8)), P, BIG, None)),
+    (UNSUPPORTED, lambda L: L.egt_logits_rules(C.byref(rules(history_width=(1 << 29) + 1, ld_history=BIG)), None)),
+    (UNSUPPORTED, lambda L: L.egt_logits_rules(C.byref(rules(n_bias=(1 << 29) + 1)), None))])
+def test_sizes_past_what_a_kernel_counts(status, call):
+    assert call(egt.lib()) == status
+
+
 # ---------------------------------------------------------------- the references themselves, on numbers worked out by hand
 def test_reference_of_slots():
     lens, counts = np.array([3, 0, 4]), np.array([2, 1, 4])
