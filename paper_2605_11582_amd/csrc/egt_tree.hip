@@ -86,6 +86,7 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
   constexpr int AHEAD = ahead_of(WR);
   extern __shared__ __align__(16) uint8_t lds[];
   __shared__ int odd_seen[W];
+  __shared__ uint64_t masks[EGT_MAX_TREE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g4 = lane >> 4;
   const int wr = wave % WR, wk = wave / WR, dim = a.c.dim;
   const int r = blockIdx.z, kh = blockIdx.y / a.row_blocks, rb = blockIdx.y % a.row_blocks;
@@ -210,6 +211,17 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
   Pages pages[AHEAD];
 #pragma unroll
   for (int j = 0; j < AHEAD; ++j) pages[j] = pages_of(j);
+  // Q^T as the B operand: lane (g, n) holds d = 32 c + 8 g .. + 7 of row n (a row past the last: the last one again, which nobody
+  // stores).  Requested behind the first page numbers, without a branch and looked at last: a wait each costs a workgroup's start XX us.
+  u4 q[NR][DC];
+#pragma unroll
+  for (int x = 0; x < NR; ++x) {
+    const int row = min(base + 16 * x + n16, rows - 1), tok = row / a.group;
+    const uint16_t *qp = a.b.q + (int64_t)(t0 + tok) * a.b.q_row + (int64_t)(kh * a.group + row - tok * a.group) * a.b.q_head;
+#pragma unroll
+    for (int c = 0; c < DC; ++c) q[x][c] = *(const u4 *)(qp + (32 * c + 8 * g4 < dim ? 32 * c + 8 * g4 : 0));
+  }
+  const uint64_t mask = a.b.mask[t0 + min((int)threadIdx.x, n - 1)];
 #pragma unroll
   for (int j = 0; j < AHEAD; ++j) {
     kring[j] = request_k(j, pages[j]);
@@ -217,24 +229,13 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
     pages[j] = pages_of(j + AHEAD);
   }
   if (threadIdx.x < W) odd_seen[threadIdx.x] = 0;
-
-  // Q^T as the B operand: lane (g, n) holds d = 32 c + 8 g .. + 7 of row n
-  h8 q[NR][DC];
+  if (threadIdx.x < EGT_MAX_TREE) masks[threadIdx.x] = mask;
 #pragma unroll
-  for (int x = 0; x < NR; ++x) {
-    const int row = base + 16 * x + n16, tok = row / a.group;
-    const uint16_t *qp = a.b.q + (int64_t)(t0 + tok) * a.b.q_row + (int64_t)(kh * a.group + row - tok * a.group) * a.b.q_head;
+  for (int x = 0; x < NR; ++x)
 #pragma unroll
-    for (int c = 0; c < DC; ++c) {
-      u4 v = {0, 0, 0, 0};
-      if (row < rows && 32 * c + 8 * g4 < dim) {
-        v = *(const u4 *)(qp + 32 * c + 8 * g4);
+    for (int c = 0; c < DC; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] ^= a.flip;
-      }
-      q[x][c] = __builtin_bit_cast(h8, v);
-    }
-  }
+      for (int e = 0; e < 4; ++e) q[x][c][e] = 32 * c + 8 * g4 < dim ? q[x][c][e] ^ a.flip : 0;
   f4 o[NR][2 * DC], l[NR];                            // weighted sums; sums
   float ref[NR], off[NR];                             // reference (base 2), SHIFT - reference
   const _Float16 one = 1;
@@ -248,7 +249,7 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
     for (int d = 0; d < 2 * DC; ++d) o[x][d] = f4{0, 0, 0, 0};
   }
 
-  __syncthreads();                                    // (odd_seen)
+  lds_barrier();                                      // (odd_seen, masks)
 
   auto compute = [&](int i) {
       const int t = tile_of(i), limit = limit_of(i);
@@ -272,7 +273,7 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
 #pragma unroll
         for (int x = 0; x < NR; ++x)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, k[h][c]), q[x][c], s[x][h], 0, 0, 0);
+          for (int h = 0; h < 2; ++h) s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, k[h][c]), __builtin_bit_cast(h8, q[x][c]), s[x][h], 0, 0, 0);
       // V^T as the A operand: lane j of a group of 16 addresses 8 bytes of key 4 g + j / 4, and gets d = 16 dt + n of keys 4 g .. 4 g + 3
       constexpr int FAR = 4;
       u4 v[FAR];
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
 #pragma unroll
         for (int x = 0; x < NR; ++x) {
           const int row = base + 16 * x + n16;
-          const uint32_t word = !drafted ? ~0u : row < rows ? (uint32_t)(a.b.mask[t0 + row / a.group] >> ((t - sp.ctx_tiles) * TILE)) : 0u;
+          const uint32_t word = !drafted ? ~0u : row < rows ? (uint32_t)(masks[row / a.group] >> ((t - sp.ctx_tiles) * TILE)) : 0u;
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -383,7 +384,7 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
 #pragma unroll
       for (int x = 0; x < NR; ++x) {
         const int row = base + 16 * x + n16;
-        if (row >= rows || !(a.b.mask[t0 + row / a.group] >> key & 1)) continue;
+        if (row >= rows || !(masks[row / a.group] >> key & 1)) continue;
 #pragma unroll
         for (int d = 0; d < 2 * DC; ++d) {
           const int at = 16 * d + 4 * g4;
