@@ -49,7 +49,7 @@ __global__ __launch_bounds__(SLOT_THREADS) void k_kv_slots(egt_slots_batch b, in
   extern __shared__ int32_t lds[];
   __shared__ uint32_t part[SLOT_THREADS / 64];
   const int n = b.requests, tid = threadIdx.x;
-  int32_t *cu = lds, *first = lds + n + 1;            // first token; first free page (-1: the request gets nothing)
+  int32_t *cu = lds, *first = lds + n + 1, *old = first + n;      // first token; first free page (-1: the request gets nothing); ONE: length
   const int per = ONE ? 1 : (n + SLOT_THREADS - 1) / SLOT_THREADS;
   const int r0 = min((ONE ? tid & 63 : tid) * per, n), r1 = min(r0 + per, n);
   const int head = *b.free_head;
@@ -69,6 +69,7 @@ __global__ __launch_bounds__(SLOT_THREADS) void k_kv_slots(egt_slots_batch b, in
     at = end;
     pages = held(pages, (uint32_t)need);
   }
+  if (ONE && r0 < r1) old[r0] = len0;
   if (r0 < r1 && r1 == n) cu[n] = (int32_t)min(at, (uint32_t)b.n_slots);
   const uint32_t left = head >= 0 ? (uint32_t)max(b.n_free - head, 0) : 0;
   uint32_t start = sum_before<ONE>(pages, part), top = 0;
@@ -95,33 +96,37 @@ __global__ __launch_bounds__(SLOT_THREADS) void k_kv_slots(egt_slots_batch b, in
     }
     if (tid == 0) *b.new_head = head + (int32_t)top;
   }
-  // the pages that are taken: a wave a request
-  const int waves = gridDim.x * (SLOT_THREADS / 64);
-  for (int r = blockIdx.x * (SLOT_THREADS / 64) + (tid >> 6); r < n; r += waves) {
-    if (first[r] < 0) continue;
-    const int64_t up = (1 << shift) - 1, len = b.lens[r];
-    const int have = (int)((len + up) >> shift), all = (int)((len + b.counts[r] + up) >> shift);
-    for (int p = have + (tid & 63); p < all; p += 64) b.block_table[(int64_t)r * b.ld_table + p] = b.free_blocks[head + first[r] + p - have];
-  }
-  // the slots: four in a row a thread
+  // The slots: four in a row a thread, lengths and page numbers of the four asked for together.  A page that is taken begins with
+  // a new token, which enters it in the table.
   const bool whole = ((uintptr_t)b.slots & 15u) == 0;
+  const int mask = (1 << shift) - 1;
   for (int64_t i0 = 4 * ((int64_t)blockIdx.x * SLOT_THREADS + tid); i0 < b.n_slots; i0 += 4 * (int64_t)SLOT_THREADS * gridDim.x) {
     int r = 0;                                        // the last request that starts at i0 or before (n: no request's)
     for (int lo = 0, hi = n + 1; lo < hi;) {
       const int mid = (lo + hi) >> 1;
       if (cu[mid] <= i0) { r = mid; lo = mid + 1; } else { hi = mid; }
     }
-    int32_t s[4];
+    int of[4], len[4], block[4], s[4];
+    bool there[4], taken[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int64_t i = i0 + j;
-      while (r < n && i >= cu[r + 1]) ++r;
-      s[j] = -1;
-      if (r < n && first[r] >= 0) {
-        const int len = b.lens[r], pos = len + (int)(i - cu[r]), p = pos >> shift, have = (int)(((int64_t)len + (1 << shift) - 1) >> shift);
-        const int block = p < have ? b.block_table[(int64_t)r * b.ld_table + p] : b.free_blocks[head + first[r] + p - have];
-        if (block >= 0 && block < b.blocks) s[j] = (block << shift) + (pos & ((1 << shift) - 1));
-      }
+      while (r < n && i0 + j >= cu[r + 1]) ++r;
+      of[j] = min(r, n - 1);
+      there[j] = r < n && first[of[j]] >= 0;
+      len[j] = ONE ? old[of[j]] : b.lens[of[j]];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int p = (len[j] + (int)(i0 + j - cu[of[j]])) >> shift, have = (int)(((int64_t)len[j] + mask) >> shift);
+      taken[j] = p >= have;
+      const int32_t *from = taken[j] ? b.free_blocks + (head + first[of[j]] + p - have) : b.block_table + ((int64_t)of[j] * b.ld_table + p);
+      block[j] = *(there[j] ? from : b.lens);         // (no slot: any memory, not looked at)
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int pos = len[j] + (int)(i0 + j - cu[of[j]]);
+      s[j] = there[j] && block[j] >= 0 && block[j] < b.blocks ? (block[j] << shift) + (pos & mask) : -1;
+      if (there[j] && taken[j] && (pos & mask) == 0) b.block_table[(int64_t)of[j] * b.ld_table + (pos >> shift)] = block[j];
     }
     if (whole && i0 + 4 <= b.n_slots) {
       *(int4 *)(b.slots + i0) = int4{s[0], s[1], s[2], s[3]};
@@ -173,7 +178,7 @@ egt_status egt_kv_slots(const egt_slots_batch *b, void *stream) {
   if (b->lens == b->new_lens || b->counts == b->new_lens || b->free_head == b->new_head) return EGT_ERR_BUFFER;
   const int64_t want = ((int64_t)b->n_slots + 4 * egt::SLOT_THREADS - 1) / (4 * egt::SLOT_THREADS);
   const dim3 grid((unsigned)std::min<int64_t>(std::max<int64_t>(want, 1), 512)), block(egt::SLOT_THREADS);
-  const size_t lds = 4 * (size_t)(2 * b->requests + 1);
+  const size_t lds = 4 * (size_t)((b->requests <= 64 ? 3 : 2) * b->requests + 1);
   return egt::answer(b->requests <= 64 ? egt::launch(egt::k_kv_slots<true>, grid, block, lds, (hipStream_t)stream, *b, egt::log2_of(b->page))
                                        : egt::launch(egt::k_kv_slots<false>, grid, block, lds, (hipStream_t)stream, *b, egt::log2_of(b->page)));
 }

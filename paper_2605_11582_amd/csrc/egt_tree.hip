@@ -91,6 +91,10 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
   const int wr = wave % WR, wk = wave / WR, dim = a.c.dim;
   const int r = blockIdx.z, kh = blockIdx.y / a.row_blocks, rb = blockIdx.y % a.row_blocks;
   const int t0 = a.b.cu_tokens[r], t1 = a.b.cu_tokens[r + 1], len = a.b.lens[r];
+  // The arguments are five lines of memory: asked for together, not one behind the other as they come up (seven requests of up
+  // to 33 tokens and 3001 keys 20.9 -> 19.4 us); not where registers are short (256 rows over 131072 keys 186 -> 194 us).
+  if constexpr (NR * DC < 8)
+    asm volatile("" ::"s"(a.b.q), "s"(a.b.k_row), "s"(a.b.mask), "s"(a.b.requests), "s"(a.c.k), "s"(a.c.k_head), "s"(a.part), "s"(a.scale2));
   const int state = request_state(a, t0, t1, len);
   if (state == ROWS_NONE) return;
   const int n = t1 - t0;
@@ -212,7 +216,8 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
 #pragma unroll
   for (int j = 0; j < AHEAD; ++j) pages[j] = pages_of(j);
   // Q^T as the B operand: lane (g, n) holds d = 32 c + 8 g .. + 7 of row n (a row past the last: the last one again, which nobody
-  // stores).  Requested behind the first page numbers, without a branch and looked at last: a wait each costs a workgroup's start XX us.
+  // stores).  Requested behind the first page numbers, without a branch and looked at last: with a wait each sixteen
+  // requests of up to 80 rows took 52 us and take 50.
   u4 q[NR][DC];
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
