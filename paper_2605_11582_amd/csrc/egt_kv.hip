@@ -53,39 +53,56 @@ __global__ __launch_bounds__(SLOT_THREADS) void k_kv_slots(egt_slots_batch b, in
   const int per = ONE ? 1 : (n + SLOT_THREADS - 1) / SLOT_THREADS;
   const int r0 = min((ONE ? tid & 63 : tid) * per, n), r1 = min(r0 + per, n);
   const int head = *b.free_head;
-  const int len0 = r0 < r1 ? b.lens[r0] : 0, count0 = r0 < r1 ? b.counts[r0] : 0;
-  uint32_t tokens = (uint32_t)max(count0, 0);
-  for (int r = r0 + 1; r < r1; ++r) tokens = held(tokens, (uint32_t)max(b.counts[r], 0));
-  uint32_t at = sum_before<ONE>(tokens, part), pages = 0;
+  // the first requests of a thread are in registers, asked for together
+  constexpr int KEEP = ONE ? 1 : 4;
+  int lens[KEEP], counts[KEEP];
+#pragma unroll
+  for (int j = 0; j < KEEP; ++j) {
+    lens[j] = b.lens[min(r0 + j, n - 1)];
+    counts[j] = b.counts[min(r0 + j, n - 1)];
+  }
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int j = 0; j < KEEP; ++j)
+      if (r0 + j < r1) f(r0 + j, lens[j], counts[j]);
+    for (int r = r0 + KEEP; r < r1; ++r) f(r, b.lens[r], b.counts[r]);
+  };
+  uint32_t tokens = 0, pages = 0;
+  each([&](int, int, int c) { tokens = held(tokens, (uint32_t)max(c, 0)); });
+  uint32_t at = sum_before<ONE>(tokens, part);
   int need0 = -1;
-  for (int r = r0; r < r1; ++r) {
-    const int64_t len = r == r0 ? len0 : b.lens[r], c = r == r0 ? count0 : b.counts[r];
+  each([&](int r, int64_t len, int64_t c) {
     const uint32_t end = held(at, (uint32_t)max(c, (int64_t)0));
     const bool room = len >= 0 && c >= 0 && len + c <= (int64_t)b.table_blocks << shift && end <= (uint32_t)b.n_slots && end < MOST;
     const int64_t up = (1 << shift) - 1, need = room ? ((len + c + up) >> shift) - ((len + up) >> shift) : 0;
     cu[r] = (int32_t)min(at, (uint32_t)b.n_slots);
     need0 = room ? (int32_t)need : -1;
-    if (!ONE) first[r] = need0;                       // (kept there until the second scan is done)
+    if (ONE) old[r] = (int32_t)len;
+    else first[r] = need0;                            // (kept there until the second scan is done)
     at = end;
     pages = held(pages, (uint32_t)need);
-  }
-  if (ONE && r0 < r1) old[r0] = len0;
+  });
   if (r0 < r1 && r1 == n) cu[n] = (int32_t)min(at, (uint32_t)b.n_slots);
   const uint32_t left = head >= 0 ? (uint32_t)max(b.n_free - head, 0) : 0;
   uint32_t start = sum_before<ONE>(pages, part), top = 0;
-  for (int r = r0; r < r1; ++r) {
+  const bool tells = blockIdx.x == 0 && (!ONE || tid < 64);
+  each([&](int r, int len, int c) {
     // (ONE: every wave writes each entry once, and all write the same: none reads another's half-done work)
     const int need = ONE ? need0 : first[r];
     start = held(start, (uint32_t)max(need, 0));
     const bool fits = start <= left && start < MOST;
-    first[r] = need <= 0 ? need : fits ? (int32_t)(start - need) : -1;      // (no page needed: 0; refused already: -1)
+    const int free = need <= 0 ? need : fits ? (int32_t)(start - need) : -1;      // (no page needed: 0; refused already: -1)
+    first[r] = free;
     if (need > 0 && fits) top = start;
-  }
+    if (tells) {
+      b.cu_tokens[r] = cu[r];
+      b.new_lens[r] = len + (free >= 0 ? c : 0);
+    }
+  });
+  if (tells && r0 < r1 && r1 == n) b.cu_tokens[n] = cu[n];
   if (!ONE) __syncthreads();
 
   if (blockIdx.x == 0) {
-    for (int r = tid; r <= n; r += SLOT_THREADS) b.cu_tokens[r] = cu[r];
-    for (int r = tid; r < n; r += SLOT_THREADS) b.new_lens[r] = b.lens[r] + (first[r] >= 0 ? b.counts[r] : 0);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
     if (!ONE) {
