@@ -193,8 +193,9 @@ egt_status egt_kv_slots(const egt_slots_batch *b, void *stream) {
                         (const void *)b->slots, (const void *)b->cu_tokens, (const void *)b->new_lens, (const void *)b->new_head})
     if (!egt::whole4(p)) return EGT_ERR_BUFFER;
   if (b->lens == b->new_lens || b->counts == b->new_lens || b->free_head == b->new_head) return EGT_ERR_BUFFER;
+  // (a million slots: 1024 workgroups, each once through its chain, 6.7 us; 512, twice through the last part, 7.7)
   const int64_t want = ((int64_t)b->n_slots + 4 * egt::SLOT_THREADS - 1) / (4 * egt::SLOT_THREADS);
-  const dim3 grid((unsigned)std::min<int64_t>(std::max<int64_t>(want, 1), 512)), block(egt::SLOT_THREADS);
+  const dim3 grid((unsigned)std::min<int64_t>(std::max<int64_t>(want, 1), 1024)), block(egt::SLOT_THREADS);
   const size_t lds = 4 * (size_t)((b->requests <= 64 ? 3 : 2) * b->requests + 1);
   return egt::answer(b->requests <= 64 ? egt::launch(egt::k_kv_slots<true>, grid, block, lds, (hipStream_t)stream, *b, egt::log2_of(b->page))
                                        : egt::launch(egt::k_kv_slots<false>, grid, block, lds, (hipStream_t)stream, *b, egt::log2_of(b->page)));

@@ -311,7 +311,7 @@ egt_status egt_logits_rules(const egt_rules_batch *b, void *stream) {
     if ((uintptr_t)p & 3) return EGT_ERR_BUFFER;
   // Slices of 4096 ids count a history in fewer workgroups; where rows are few, slices of 1024 have the whole chip at work.  Rows of one
   // request share a count: as many together as a request has on average, as long as there are 2048 workgroups (128 rows of
-  // 128000 ids, 72 of them used: 1024 workgroups 23.5 us, 2048 19.8, 4096 26.3; slices of 2048 21.2; of 8192 with 8 waves 22.5).
+  // 128000 ids, 72 of them used: 1024 workgroups 19.1 us, 2048 16.0, 4096 18.8).
   const bool large = (int64_t)b->tokens * ((b->vocab + 4095) / 4096) >= 512;
   const int slices = large ? (b->vocab + 4095) / 4096 : (b->vocab + 1023) / 1024;
   const int64_t each = std::min<int64_t>((int64_t)b->tokens * slices / 2048, (b->tokens + b->requests - 1) / b->requests);

@@ -370,6 +370,16 @@ def test_adapters(M, cols, rows, rank, n, pad):
     check_lora(lora_case(np.random.default_rng(M * 1000 + cols), M, cols, rows, rank, n, pad=pad))
 
 
+@pytest.mark.parametrize("rows,rank,pad", [(4096, 32, 0), (4100, 64, 1), (8192, 128, 0), (4099, 16, 0)])
+def test_adapters_of_many_tokens_and_rows(rows, rank, pad):
+    rng = np.random.default_rng(rows)
+    index = rng.integers(-1, 65, 64)                      # none, one past the last, and tokens that share one
+    index[40:60] = 7
+    c = lora_case(rng, 64, 64, rows, rank, 64, index.tolist(), pad=pad)
+    check_lora(c)
+    check_lora(c, base=False)
+
+
 def test_adapters_one_for_all_none_for_all_and_without_options():
     rng = np.random.default_rng(20)
     for index in ([2] * 64, [-1] * 64, list(range(64)), [-5, 3] * 32):
@@ -466,6 +476,13 @@ def check_rules(c, logits, buf, out, leave=(), what=""):
     ([1] * 70, 2049, 100, "fp16", 7), ([4, 4], 50257, 2000, "fp16", 0), ([2], 128000, 9000, "fp16", 0), ([2, 1], 100001, 513, "fp32", 0), ([7], 8192, 4096, "fp16", 8)])
 def test_rules(counts, vocab, length, kind, pad):
     check_rules(*rules_case(np.random.default_rng(vocab + length), counts, vocab, length, kind, pad=pad))
+
+
+@pytest.mark.parametrize("counts,vocab,length,kind", [
+    ([1, 0, 2] * 1700, 45, 8, "fp16"), ([2] * egt.MAX_REQUESTS, 9, 3, "fp32"), ([64, 1, 0, 64, 60, 64], 100003, 5000, "fp16"), ([64, 3, 64, 61], 131072, 60, "fp32")])
+def test_rules_of_many_requests_and_rows(counts, vocab, length, kind):
+    """Requests by the thousand, and several rows a workgroup that change from request to request."""
+    check_rules(*rules_case(np.random.default_rng(vocab), counts, vocab, length, kind, n_bias=300 if vocab > 1000 else 5))
 
 
 @pytest.mark.parametrize("leave", [("history", "history_len", "prompt_len"), ("prompt_len",), ("draft", "mask"), ("repetition",), ("frequency",), ("presence",),
