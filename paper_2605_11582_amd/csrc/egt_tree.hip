@@ -15,10 +15,10 @@
 //                  V^T comes out of LDS by the transposing read; the sum of p is one more product, with ones.
 //
 // What bounds it: with up to 64 rows a key head the cache's bytes (16 rows over 131072 keys, 8 heads of 128: 107 us, 5.0 TB/s;
-// 64 rows 116 us), above that the steps themselves, of which one wave a SIMD can hide little: 256 rows 187 us, 2.9 TB/s and
+// 64 rows 116 us), above that the steps themselves, of which one wave a SIMD can hide little: 256 rows 183 us, 2.9 TB/s and
 // 0.73 PFLOP/s, matrix units busy 38 % of the time and vector units 46 %.  A wave of two row tiles spends, of 2500 cycles a step,
 // 345 on staging, 500 on addresses and requests, 610 on scores (256 of them products), 390 on weights and 555 on sums (288).  Short
-// contexts are bound by a launch and the chain lengths - page numbers - keys, 9 us, and a launch more where there are several spans.
+// contexts are bound by a launch and the chain lengths - page numbers - keys, 8.4 us, and a launch more where there are several spans.
 #include "egt_mfma_common.h"
 #include "egt_serve.h"
 
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
   for (int j = 0; j < AHEAD; ++j) pages[j] = pages_of(j);
   // Q^T as the B operand: lane (g, n) holds d = 32 c + 8 g .. + 7 of row n (a row past the last: the last one again, which nobody
   // stores).  Requested behind the first page numbers, without a branch and looked at last: with a wait each sixteen
-  // requests of up to 80 rows took 52 us and take 50.
+  // requests of up to 80 rows took 52 us and take 51.
   u4 q[NR][DC];
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
