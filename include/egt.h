@@ -525,7 +525,7 @@ egt_status egt_tree_attention(const egt_tree_batch *b, const egt_kv_cache *cache
  * result, NULL for zeros; it may be Y itself (same ldbase and ldy), and must not overlap Y otherwise.  scale: one FP32
  * per adapter, NULL for ones.  index[m] < 0: no adapter, Y[m] = base[m]; index[m] >= adapters:
  * NaN.  Any token may have any adapter, and tokens of one adapter read it once.
- * FP32 sums in a fixed order; A . X[m] goes on as two FP16 numbers that hold 22 of its bits.
+ * FP32 sums in a fixed order; A . X[m] goes on in 22 bits of every entry at least, however far apart its entries are.
  * What is not finite in an adapter gives infinities or NaN in its own tokens alone.
  * cols and rank multiples of 8, rank <= 128, cols and rows <= 2^30, adapters >= 1; X, A, B, a_stride, b_stride and ldx whole 16 bytes.
  * Workspace as for egt_tree_attention; egt_lora_smallm_ws_bytes is the HOST query. */

@@ -421,6 +421,52 @@ def test_adapters_past_the_last_and_large_numbers():
     check_lora(c)
 
 
+def apart(c, large, small):
+    """Every third rank `large`, and B zero there: the result is that of the ranks that are `small` times as large or less."""
+    rank = c["A"].shape[1]
+    c["A"] *= dev(np.where(np.arange(rank) % 3 == 0, large, small * 0.5 ** (np.arange(rank) % 7)).astype(np.float16))[None, :, None]
+    c["B"][:, :, ::3] = 0
+    c["B"] *= 2000
+    c["base"].mul_(2.0 ** -10)
+    return c
+
+
+@pytest.mark.parametrize("large,small", [(2.0 ** 12, 2.0 ** -8), (2.0 ** 15, 2.0 ** -12)])
+@pytest.mark.parametrize("M,rows,rank", [(1, 40, 8), (3, 333, 24), (20, 4100, 32), (64, 300, 64), (17, 500, 128)])
+def test_adapters_whose_ranks_differ_in_size(M, rows, rank, large, small):
+    c = apart(lora_case(np.random.default_rng(rank), M, 512, rows, rank, 3), large, small)
+    check_lora(c)
+    check_lora(c, base=False)
+
+
+def test_a_token_whose_ranks_lie_far_apart_beside_others():
+    """What one token needs, an infinity among it, changes no bit of the other tokens of its adapter."""
+    rng = np.random.default_rng(24)
+    c = lora_case(rng, 40, 512, 200, 24, 1, [0] * 40)
+    c["X"][7] = 0
+    c["X"][7, 0], c["A"][0, 1, 0] = 60000, 6e-8
+    check_lora(c)
+    alone = c["Y"].clone()
+    c["X"][9, 3] = float("inf")
+    egt.lora_smallm(c["X"], c["A"], c["B"], dev(c["index"]), c["Y"], c["ws"], base=c["base"], scale=dev(c["scale"]))
+    ok = np.isfinite(c["Y"].cpu().numpy())
+    others = np.arange(40) != 9
+    assert not ok[9].any() and ok[others].all()
+    assert np.array_equal(c["Y"].cpu().numpy()[others], alone.cpu().numpy()[others])
+
+
+def test_adapters_of_a_small_rank_beside_a_large_one():
+    torch = G.torch_mod()
+    X, A, B, Y = (torch.zeros(s, dtype=torch.float16, device="cuda") for s in ((1, 8), (1, 8, 8), (1, 4, 8), (1, 4)))
+    ws = torch.zeros(egt.lora_smallm_ws_bytes(X, A), dtype=torch.uint8, device="cuda")
+    X[0, 0], A[0, 0, 0], A[0, 1, 1] = 30000, 1, 1
+    for small, weight in ((3e-4, 1000), (0.01, 1000), (6e-8, 60000), (0.7, 1)):
+        X[0, 1], B[0, :, 1] = small, weight
+        egt.lora_smallm(X, A, B, dev(np.zeros(1, np.int32)), Y, ws)
+        want = (X[0, 1].double() * weight).half()
+        assert bool((Y == want).all()), (small, Y, want)
+
+
 def test_an_infinity_stays_with_its_token():
     rng = np.random.default_rng(23)
     c = lora_case(rng, 20, 256, 100, 16, 2, [0, 1] * 10)
