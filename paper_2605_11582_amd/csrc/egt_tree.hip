@@ -31,6 +31,9 @@ constexpr int TILE = 32;             // keys a wave takes at a time
 // p is held as 2^SHIFT p against its reference, and may pass it by 2^SLACK: 2^15 at most in FP16, and whole
 // precision down to 2^-24 of the largest weight.
 constexpr float SHIFT = 10.f, SLACK = 5.f, EXP2_LIMIT = 32768.f;
+// From here on the sum of an exponent and SHIFT is too coarse for one multiply-add against the reference (its steps pass what FP16 holds,
+// from 2^24 on, and then SHIFT itself): the difference of the scores is taken first.
+constexpr float FAR_SCORE = 0x1p20f;
 
 struct TreeArgs {
   egt_tree_batch b;
@@ -242,7 +245,7 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
 #pragma unroll
       for (int e = 0; e < 4; ++e) q[x][c][e] = 32 * c + 8 * g4 < dim ? q[x][c][e] ^ a.flip : 0;
   f4 o[NR][2 * DC], l[NR];                            // weighted sums; sums
-  float ref[NR], off[NR];                             // reference (base 2), SHIFT - reference
+  float ref[NR], off[NR];                             // reference (a score); SHIFT - the reference as an exponent of 2, or infinite
   const _Float16 one = 1;
   const h8 ones = {one, one, one, one, one, one, one, one};
 #pragma unroll
@@ -308,8 +311,8 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
             }
         }
       }
-      // Scores that pass the reference too far show in p itself, whose bits order as whole numbers do (no reference yet: off
-      // is infinite, and so is p, or NaN).
+      // Scores that pass the reference too far show in p itself, whose bits order as whole numbers do (no reference yet, or one whose
+      // exponent is FAR_SCORE or more: off is infinite, and so is p, or NaN).
       float e[NR][8];
       uint32_t most = 0;
 #pragma unroll
@@ -324,12 +327,14 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
         for (int x = 0; x < NR; ++x) {
           float top = fmaxf(fmaxf(fmaxf(s[x][0][0], s[x][0][1]), fmaxf(s[x][0][2], s[x][0][3])), fmaxf(fmaxf(s[x][1][0], s[x][1][1]), fmaxf(s[x][1][2], s[x][1][3])));
           top = fmaxf(top, __shfl_xor(top, 16, 64));
-          top = fmaxf(top, __shfl_xor(top, 32, 64)) * a.scale2;
-          const float to = top > ref[x] + SLACK ? top : ref[x];
-          const float f = ref[x] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[x] - to);     // (nothing is there yet)
+          top = fmaxf(top, __shfl_xor(top, 32, 64));
+          const float to = (top - ref[x]) * a.scale2 > SLACK ? top : ref[x], was2 = ref[x] * a.scale2, to2 = to * a.scale2;
+          const bool none = to2 == -INFINITY, far = !none && fabsf(to2) >= FAR_SCORE;
+          // (nothing is there yet: 1)
+          const float f = was2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(far ? (ref[x] - to) * a.scale2 : was2 - to2);
           ref[x] = to;
-          off[x] = to == -INFINITY ? INFINITY : SHIFT - to;
-          const float now = to == -INFINITY ? SHIFT : off[x];
+          off[x] = none || far ? INFINITY : SHIFT - to2;
+          const float from = far ? to : 0.f, now = none || far ? SHIFT : off[x];
 #pragma unroll
           for (int j = 0; j < 4; ++j) l[x][j] *= f;
 #pragma unroll
@@ -337,7 +342,7 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[x][d][j] *= f;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) e[x][j] = __builtin_amdgcn_exp2f(fmaf(s[x][j >> 2][j & 3], a.scale2, now));
+          for (int j = 0; j < 8; ++j) e[x][j] = __builtin_amdgcn_exp2f(fmaf(s[x][j >> 2][j & 3] - from, a.scale2, now));
         }
       }
       h8 p[NR];
@@ -375,7 +380,7 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
     if (g4 == 0) {
-      refs[wave][16 * x + n16] = ref[x];
+      refs[wave][16 * x + n16] = ref[x] * a.scale2;   // (base 2)
       sums[wave][16 * x + n16] = l[x][0];
     }
   }
@@ -416,7 +421,7 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
       // (a wave without a reference has no weight, or only NaN: it keeps what it has)
       total += (rw == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(rw - safe_top)) * sums[WR * w + wr][16 * x + n16];
     }
-    const float f = ref[x] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[x] - safe_top);
+    const float ref2 = ref[x] * a.scale2, f = ref2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref2 - safe_top);
     if (WK > 1) {
       float *area = (float *)(lds + wave * KV);
       // row n of 16, d back to back; rows are shifted by their number so that a store of 16 rows spreads over the banks

@@ -193,6 +193,19 @@ def test_attention_of_large_scores():
     check_tree(tree_case(np.random.default_rng(5), [300, 20], [9, 40], 8, 2, 128, 16, scale=6.0))
 
 
+@pytest.mark.parametrize("scale", [0.05, 0.3, 1.0, -7.0, 1e3, -1e6])
+def test_attention_of_scores_past_whole_numbers(scale):
+    """Scores from 2^20 on, up to 2^50: still weights between 0 and 1 that sum to 1."""
+    for lens, counts, heads, kv_heads, dim in (([70, 0, 301], [5, 40, 1], 4, 2, 128), ([900], [2], 2, 2, 64), ([33], [64], 16, 4, 128), ([6000], [3], 4, 2, 96)):
+        c = tree_case(np.random.default_rng(31), lens, counts, heads, kv_heads, dim, 16, scale=3000.0)
+        c["k_cache"].mul_(3000)
+        c["v"].copy_(c["v"] / 3000)
+        c["scale"] = scale
+        check_tree(c, scale)
+        got, seen = c["out"][:int(c["cu"][-1])].float(), max(float(c["v"].abs().max()), float(c["v_cache"].abs().max()))
+        assert float(got.abs().max()) <= seen and bool((got != 0).any(-1).all())
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.0, 1e-40, -0.125, -3.0])
 def test_attention_of_other_scales(scale):
     """Every visible key weighs the same where the scale is zero, and what is masked still does not enter."""
