@@ -555,7 +555,8 @@ egt_status egt_lora_smallm(const egt_lora_batch *b, void *workspace, size_t work
  * of allowed[allowed_row[i]][t / 32] decides (n_allowed rows, ld_allowed words apart; an
  * allowed_row past the last gives NaN in the row).
  * Any of history (with both lengths), draft (with mask), repetition, frequency, presence, bias_ids
- * (with bias) and allowed (with allowed_row) may be NULL: that rule is left out, and a prompt_len of NULL is no prompt.
+ * (with bias) and allowed (with allowed_row, both or neither) may be NULL: that rule is left out, and a prompt_len of NULL is
+ * no prompt.  A grammar without rows (n_allowed 0) has an address of its own all the same; it is not read.
  * kind: EGT_LOGITS_FP16 or EGT_LOGITS_FP32, of logits and out.  out may be logits itself (same
  * leading dimension) and must not overlap it otherwise.  Up to 64 tokens a request see each other: bits past a
  * request's tokens are passed over.  requests <= EGT_MAX_REQUESTS, tokens <= 65535, vocab <= 2^30,

@@ -333,9 +333,10 @@ struct Rules {
     if (a[13] != Py_None) {
       const at::Tensor &m = r.rows(a[13], "allowed", at::kInt, b.ld_allowed);
       r.same("allowed: words a row", m.size(1), (vocab + 31) / 32);
-      b.allowed = (const uint32_t *)m.data_ptr();
       b.n_allowed = r.fits("allowed", m.size(0));
       b.allowed_row = r.vec<const int32_t>(a[14], "allowed_row", at::kInt, tokens);
+      // (a grammar without rows has no memory, and is not the same as none: no row may be asked for.  It gets an address that is not read.)
+      b.allowed = b.n_allowed ? (const uint32_t *)m.data_ptr() : (const uint32_t *)b.allowed_row;
     }
   }
   int launch(void *s) const { return V.rules(&b, s); }

@@ -301,7 +301,7 @@ egt_status egt_logits_rules(const egt_rules_batch *b, void *stream) {
   if (b->requests > EGT_MAX_REQUESTS || b->tokens > 65535 || b->vocab > (1 << 30) || b->history_width > (1 << 29) || b->n_bias > (1 << 29)) return EGT_ERR_UNSUPPORTED;
   if (b->requests == 0 || b->tokens == 0 || b->vocab == 0) return EGT_OK;
   if (!b->logits || !b->out || !b->cu_tokens || (b->history && !b->history_len) || (b->draft && !b->mask) || (b->bias_ids && !b->bias) ||
-      (b->allowed && !b->allowed_row))
+      !b->allowed != !b->allowed_row)
     return EGT_ERR_NULL;
   const uintptr_t size = b->kind == EGT_LOGITS_FP16 ? 1 : 3;
   if (((uintptr_t)b->logits & size) || ((uintptr_t)b->out & size) || ((uintptr_t)b->mask & 7)) return EGT_ERR_BUFFER;

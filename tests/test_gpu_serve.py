@@ -581,6 +581,17 @@ def test_rules_masks_that_leave_nothing_and_odd_numbers():
         assert (got[:4] == -np.inf).all() and np.isnan(got[4:6]).all()
 
 
+@pytest.mark.parametrize("kind", ["fp16", "fp32"])
+def test_rules_of_a_grammar_without_rows(kind):
+    """Every row of it is past the last: NaN, not everything allowed."""
+    c, logits, buf, out = rules_case(np.random.default_rng(6), [3, 2], 1000, 10, kind)
+    c["allowed"] = c["allowed"][:0]
+    c["allowed_row"] = np.array([-1, 0, 5, -7, 2 ** 31 - 1, 0, 0], np.int32)
+    check_rules(c, logits, buf, out)
+    got = out.cpu().numpy()
+    assert np.isnan(got[[1, 2, 4]]).all() and not np.isnan(got[[0, 3]]).any()
+
+
 def test_rules_in_place_and_bad_lengths():
     torch = G.torch_mod()
     c, logits, buf, out = rules_case(np.random.default_rng(3), [4, 8, 2], 6007, 64, "fp16")

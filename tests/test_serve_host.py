@@ -143,6 +143,12 @@ def test_logits_rules_refuses(change, status):
     assert egt.lib().egt_logits_rules(C.byref(rules(**change)), None) == status
 
 
+def test_rows_of_a_grammar_need_a_grammar():
+    """An empty grammar's missing address is not "everything is allowed"."""
+    assert egt.lib().egt_logits_rules(C.byref(rules(allowed=None, n_allowed=0)), None) == NULL
+    assert egt.lib().egt_logits_rules(C.byref(rules(allowed=None, allowed_row=None, n_allowed=0, cu_tokens=P + 2)), None) == BUFFER      # (neither: as ever)
+
+
 def test_the_binding_names_what_is_wrong():
     i, h = torch.zeros(4, dtype=torch.int32), torch.zeros((4, 2, 8), dtype=torch.float16)
     with pytest.raises(ValueError, match="lens: expected a device tensor"):
