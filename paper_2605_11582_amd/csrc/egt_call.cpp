@@ -19,7 +19,6 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 
-#include <algorithm>
 #include <cstdint>
 #include <exception>
 #include <memory>

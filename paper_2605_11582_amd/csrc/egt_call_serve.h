@@ -58,7 +58,7 @@ struct Reader {
   const at::Tensor &rows(PyObject *o, const char *name, at::ScalarType type, int64_t &ld) {
     const at::Tensor &t = tensor(o, name, type, 2);
     if (t.size(1) > 1 && t.stride(1) != 1) throw Refused{std::string(name) + ": the elements of a row must be contiguous"};
-    ld = t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1));
+    ld = t.size(0) > 1 ? t.stride(0) : t.size(1);      // (a single row has no distance to another)
     return t;
   }
   // (rows, heads, dim) with contiguous dim; strides of axes of one element do not matter

@@ -606,6 +606,26 @@ def test_rules_in_place_and_bad_lengths():
     assert (out == 5).all()
 
 
+def test_a_single_row_has_no_distance_to_another():
+    """One token's X, Y, base and logits out of wider buffers, in place under another stride."""
+    torch = G.torch_mod()
+    rng = np.random.default_rng(70)
+    a = lora_case(rng, 1, 64, 40, 8, 2, [1])
+    a["X"] = dev(f16(rng, 1, 67))[:, :64]
+    check_lora(a)
+    Y = dev(f16(rng, 1, 44))[:, :40]
+    want, bound = R.lora(*(t.cpu().numpy().astype(np.float64) for t in (a["X"], a["A"], a["B"])), a["index"], Y.cpu().numpy().astype(np.float64), np.ones(2))
+    egt.lora_smallm(a["X"], a["A"], a["B"], dev(a["index"]), Y, a["ws"], base=Y.as_strided((1, 40), (40, 1)))
+    R.close(Y.cpu().numpy(), want, bound)
+    logits = dev(f16(rng, 1, 107))[:, :100]
+    was = logits.cpu().numpy().astype(np.float64)
+    factor = np.array([1.5], np.float32)
+    history = dict(history=np.arange(0, 100, 7, dtype=np.int32)[None], history_len=np.array([9], np.int32), repetition=factor)
+    egt.logits_rules(logits, logits.as_strided((1, 100), (100, 1)), dev(np.array([0, 1], np.int32)), **{k: dev(v) for k, v in history.items()})
+    want, bound = R.rules(was, np.array([0, 1]), True, **history)
+    R.close(logits.cpu().numpy(), want, bound)
+
+
 # ---------------------------------------------------------------- together, on streams, in graphs
 def test_a_verification_step():
     """Projections, adapters, attention, slots, writing and rules, twice: the second step reads what the first has written."""
