@@ -41,15 +41,16 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t *part) {
 
 // Two running sums over the requests - tokens, then pages - decide everything, and a few thousand lengths are 16 KB: every
 // workgroup computes both for itself (each thread a run of requests, then one scan over the threads; up to 64 requests every wave
-// for itself, a lane a request) and keeps them in LDS, so that the token slots, which are the bytes, are written by the whole chip
-// without a second launch and without one workgroup waiting for another.  What binds it is that chain: lengths, two scans, a
-// search, a page number, behind a launch.
+// for itself, a lane a request, in LDS of its own) and keeps them in LDS, so that the token slots, which are the bytes, are written
+// by the whole chip without a second launch and without one workgroup waiting for another.  What binds it is that chain: lengths,
+// two scans, a search, a page number, behind a launch.
 template <bool ONE>
 __global__ __launch_bounds__(SLOT_THREADS) void k_kv_slots(egt_slots_batch b, int shift) {
   extern __shared__ int32_t lds[];
   __shared__ uint32_t part[SLOT_THREADS / 64];
   const int n = b.requests, tid = threadIdx.x;
-  int32_t *cu = lds, *first = lds + n + 1, *old = first + n;      // first token; first free page (-1: the request gets nothing); ONE: length
+  int32_t *cu = lds + (ONE ? (tid >> 6) * (3 * n + 1) : 0), *first = cu + n + 1, *old = first + n;
+  // (first token; first free page, -1: the request gets nothing; ONE: length)
   const int per = ONE ? 1 : (n + SLOT_THREADS - 1) / SLOT_THREADS;
   const int r0 = min((ONE ? tid & 63 : tid) * per, n), r1 = min(r0 + per, n);
   const int head = *b.free_head;
@@ -87,7 +88,6 @@ __global__ __launch_bounds__(SLOT_THREADS) void k_kv_slots(egt_slots_batch b, in
   uint32_t start = sum_before<ONE>(pages, part), top = 0;
   const bool tells = blockIdx.x == 0 && (!ONE || tid < 64);
   each([&](int r, int len, int c) {
-    // (ONE: every wave writes each entry once, and all write the same: none reads another's half-done work)
     const int need = ONE ? need0 : first[r];
     start = held(start, (uint32_t)max(need, 0));
     const bool fits = start <= left && start < MOST;
@@ -100,7 +100,13 @@ __global__ __launch_bounds__(SLOT_THREADS) void k_kv_slots(egt_slots_batch b, in
     }
   });
   if (tells && r0 < r1 && r1 == n) b.cu_tokens[n] = cu[n];
-  if (!ONE) __syncthreads();
+  if (ONE) {                                          // (the lanes of a wave read each other's entries)
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  } else {
+    __syncthreads();
+  }
 
   if (blockIdx.x == 0) {
 #pragma unroll
@@ -196,7 +202,7 @@ egt_status egt_kv_slots(const egt_slots_batch *b, void *stream) {
   // (a million slots: 1024 workgroups, each once through its chain, 6.7 us; 512, twice through the last part, 7.7)
   const int64_t want = ((int64_t)b->n_slots + 4 * egt::SLOT_THREADS - 1) / (4 * egt::SLOT_THREADS);
   const dim3 grid((unsigned)std::min<int64_t>(std::max<int64_t>(want, 1), 1024)), block(egt::SLOT_THREADS);
-  const size_t lds = 4 * (size_t)((b->requests <= 64 ? 3 : 2) * b->requests + 1);
+  const size_t lds = 4 * (size_t)(b->requests <= 64 ? egt::SLOT_THREADS / 64 * (3 * b->requests + 1) : 2 * b->requests + 1);
   return egt::answer(b->requests <= 64 ? egt::launch(egt::k_kv_slots<true>, grid, block, lds, (hipStream_t)stream, *b, egt::log2_of(b->page))
                                        : egt::launch(egt::k_kv_slots<false>, grid, block, lds, (hipStream_t)stream, *b, egt::log2_of(b->page)));
 }

@@ -232,6 +232,49 @@ def test_launches_of_tree_attention(tmp_path):
     assert len(kernels) >= 20
 
 
+OTHER_LAUNCHES = r"""
+import ctypes as C, sys
+sys.path.insert(0, {root!r})
+from paper_2605_11582_amd import binding as B
+L, P = B._declare(C.CDLL(B.LIB_PATH)), 1 << 20             # (without PyTorch)
+for requests in (1, 3, 64, 65, 1000, 8192):
+    print("case slots", requests, flush=True)
+    b = B.SlotsBatch(lens=P, counts=P, block_table=P, free_blocks=P, free_head=P, slots=P, cu_tokens=P, new_lens=2 * P, new_head=2 * P, ld_table=4, requests=requests,
+                     table_blocks=4, page=16, blocks=8, n_free=5, n_slots=7)
+    assert L.egt_kv_slots(C.byref(b), None) == 0
+"""
+
+
+@pytest.fixture(scope="module")
+def other_launches(tmp_path_factory):
+    """[(case, [(kernel, grid x, grid y, threads, LDS bytes)])]: what runs of the calls above, as a stand-in for the runtime's launch sees it."""
+    import test_kernel_routes as routes
+    cc = shutil.which("gcc")
+    if not cc:
+        pytest.skip("no host compiler")
+    d = tmp_path_factory.mktemp("launch")
+    (d / "launch.c").write_text(routes.STAND_IN)
+    subprocess.run([cc, "-shared", "-fPIC", "-O1", str(d / "launch.c"), "-o", str(d / "launch.so")], check=True)
+    env = {**os.environ, "LD_PRELOAD": " ".join(v for v in (str(d / "launch.so"), os.environ.get("LD_PRELOAD", "")) if v)}
+    out = subprocess.run([os.sys.executable, "-c", OTHER_LAUNCHES.replace("{root!r}", repr(ROOT))], capture_output=True, text=True, env=env, timeout=120)
+    assert out.returncode == 0, (out.stdout[-300:], out.stderr[-2000:])
+    seen = []
+    for line in out.stdout.splitlines():
+        word = line.split()
+        if word[0] == "case":
+            seen.append((word[1:], []))
+        else:
+            seen[-1][1].append((word[1], *(int(w) for w in word[2:])))
+    return seen
+
+
+def test_waves_of_the_slot_maps_have_lds_of_their_own(other_launches):
+    """Up to 64 requests every wave keeps offsets, pages and lengths for itself; beyond, the workgroup shares offsets and pages."""
+    for (_, requests), [(name, _, _, threads, lds)] in (c for c in other_launches if c[0][0] == "slots"):
+        n = int(requests)
+        assert lds == 4 * (threads // 64 * (3 * n + 1) if n <= 64 else 2 * n + 1), (requests, name)
+
+
 BIG = 1 << 30
 
 
