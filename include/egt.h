@@ -471,7 +471,7 @@ egt_status egt_kv_slots(const egt_slots_batch *b, void *stream);
  * row i) of k and v goes to slot slots[i], for i < n.  Entries whose slot is not one of the
  * cache's (-1: rejected, padding) or whose row is not one of the n_rows are passed over.  Element d of head h of
  * row i is at k[i * k_row + h * k_head + d]; strides as in the cache.  The slots of a call are
- * meant to be different; where two are the same, each 16 bytes are one of the two rows'.  n < 2^24. */
+ * meant to be different; where two are the same, each 16 bytes are one of the two rows'.  n < 2^24, heads * dim <= 2^33. */
 typedef struct {
   const uint16_t *k, *v;
   const int32_t *slots, *rows;        /* [n]; rows may be NULL                               */
@@ -527,7 +527,7 @@ egt_status egt_tree_attention(const egt_tree_batch *b, const egt_kv_cache *cache
  * NaN.  Any token may have any adapter, and tokens of one adapter read it once.
  * FP32 sums in a fixed order; A . X[m] goes on in 22 bits of every entry at least, however far apart its entries are.
  * What is not finite in an adapter gives infinities or NaN in its own tokens alone.
- * cols and rank multiples of 8, rank <= 128, cols and rows <= 2^30, adapters >= 1; X, A, B, a_stride, b_stride and ldx whole 16 bytes.
+ * cols and rank multiples of 8, rank <= 128, cols <= 2^30, rows <= 2^30 - 64, adapters >= 1; X, A, B, a_stride, b_stride and ldx whole 16 bytes.
  * Workspace as for egt_tree_attention; egt_lora_smallm_ws_bytes is the HOST query. */
 typedef struct {
   const uint16_t *X, *A, *B, *base;

@@ -216,8 +216,8 @@ egt_status egt_kv_append(const egt_append_batch *b, const egt_kv_cache *cache, v
   if (!b->k || !b->v || !b->slots) return EGT_ERR_NULL;
   if (!egt::whole16(b->k) || !egt::whole16(b->v) || !egt::whole8(b->k_row, b->k_head, b->v_row, b->v_head) || !egt::whole4(b->slots) || !egt::whole4(b->rows))
     return EGT_ERR_BUFFER;
-  if (b->n >= 1 << 24) return EGT_ERR_UNSUPPORTED;     // (a launch has less than 2^32 threads)
   const int64_t pieces = (int64_t)cache->heads * (cache->dim / 8);
+  if (b->n >= 1 << 24 || pieces > 1 << 30) return EGT_ERR_UNSUPPORTED;     // (a launch has less than 2^32 threads; pieces are counted in 31 bits)
   int tshift = 2;
   while (tshift < 8 && (1 << tshift) < pieces) ++tshift;
   const int64_t groups = ((int64_t)b->n + (256 >> tshift) - 1) >> (8 - tshift);

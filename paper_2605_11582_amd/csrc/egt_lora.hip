@@ -307,7 +307,7 @@ egt_status egt_lora_smallm(const egt_lora_batch *b, void *workspace, size_t work
   if (b->rows < 0 || b->adapters < 1 || b->ldx < b->cols || b->ldy < b->rows || (b->base && b->ldbase < b->rows) ||
       (b->base == b->Y && b->base && b->ldbase != b->ldy) || b->a_stride < 0 || b->b_stride < 0)
     return EGT_ERR_SHAPE;
-  if (b->rows > 1 << 30) return EGT_ERR_UNSUPPORTED;
+  if (b->rows > (1 << 30) - 64) return EGT_ERR_UNSUPPORTED;      // (a launch has less than 2^32 threads)
   if (b->rows == 0) return EGT_OK;                    // nothing to compute, pointers not examined
   if (!b->X || !b->A || !b->B || !b->Y || !b->index || !workspace) return EGT_ERR_NULL;
   if (workspace_bytes < egt::workspace_of(b->M, b->cols, b->rank)) return EGT_ERR_SHAPE;

@@ -242,6 +242,17 @@ for requests in (1, 3, 64, 65, 1000, 8192):
     b = B.SlotsBatch(lens=P, counts=P, block_table=P, free_blocks=P, free_head=P, slots=P, cu_tokens=P, new_lens=2 * P, new_head=2 * P, ld_table=4, requests=requests,
                      table_blocks=4, page=16, blocks=8, n_free=5, n_slots=7)
     assert L.egt_kv_slots(C.byref(b), None) == 0
+for rows, ld in ((1, 1), (64, 64), (2100, 2100), (4100, 4101), (11008, 11008), (65536, 65536), ((1 << 30) - 64, (1 << 30) - 64), ((1 << 30) - 64, (1 << 30) - 63),
+                 ((1 << 30) - 63, (1 << 30) - 63), (1 << 30, 1 << 30)):
+    for M, rank in ((1, 8), (64, 32), (64, 64), (64, 128)):
+        b = B.LoraBatch(X=P, A=P, B=P, base=P, Y=P, index=P, scale=P, ldx=64, ldbase=ld, ldy=ld, a_stride=512, b_stride=800, M=M, cols=64, rows=rows, rank=rank, adapters=M)
+        print("case lora", rows, M, rank, flush=True)
+        print("status", L.egt_lora_smallm(C.byref(b), P, 1 << 30, None), flush=True)
+for heads, dim, n in ((1, 8, 1), (8, 128, (1 << 24) - 1), (1 << 20, 256, 5), (1 << 25, 256, 5), (1 << 26, 256, 5), ((1 << 31) - 1, 8, 5), ((1 << 31) - 1, 256, 5)):
+    c = B.KvCache(k=P, v=P, blocks=8, heads=heads, page=16, dim=dim, k_block=2048, k_head=1024, k_token=64, v_block=2048, v_head=1024, v_token=64)
+    b = B.AppendBatch(k=P, v=P, slots=P, k_row=128, k_head=64, v_row=128, v_head=64, n=n, n_rows=n)
+    print("case append", heads, dim, flush=True)
+    print("status", L.egt_kv_append(C.byref(b), C.byref(c), None), flush=True)
 """
 
 
@@ -263,6 +274,8 @@ def other_launches(tmp_path_factory):
         word = line.split()
         if word[0] == "case":
             seen.append((word[1:], []))
+        elif word[0] == "status":
+            seen[-1] = (seen[-1][0] + [int(word[1])], seen[-1][1])
         else:
             seen[-1][1].append((word[1], *(int(w) for w in word[2:])))
     return seen
@@ -273,6 +286,19 @@ def test_waves_of_the_slot_maps_have_lds_of_their_own(other_launches):
     for (_, requests), [(name, _, _, threads, lds)] in (c for c in other_launches if c[0][0] == "slots"):
         n = int(requests)
         assert lds == 4 * (threads // 64 * (3 * n + 1) if n <= 64 else 2 * n + 1), (requests, name)
+
+
+def test_launches_of_adapters_and_cache_writes(other_launches):
+    """A grid that a launch takes (less than 2^32 threads), or EGT_ERR_UNSUPPORTED and no launch; a token's pieces are counted in 31 bits."""
+    kernels = set()
+    for (what, *sizes, status), launches in (c for c in other_launches if c[0][0] != "slots"):
+        sizes = [int(v) for v in sizes]
+        fits = sizes[0] <= (1 << 30) - 64 if what == "lora" else sizes[0] * (sizes[1] // 8) <= 1 << 30
+        assert status == (0 if fits else UNSUPPORTED) and len(launches) == ((2 if what == "lora" else 1) if fits else 0), (what, sizes)
+        for name, x, y, threads, lds in launches:
+            assert x * threads < 1 << 32 and y <= 65535, (what, sizes, name)
+            kernels.add(name)
+    assert len([k for k in kernels if "k_lora_expand" in k]) == 11
 
 
 BIG = 1 << 30
