@@ -91,6 +91,15 @@ def test_slots_that_cannot_be_had():
     check_slots(lens, counts, table, 8, blocks, free, 0, 0)                     # no slots at all
 
 
+@pytest.mark.parametrize("n,most,context,page,share", [(300, 4096, 500, 16, 0.97), (64, 20000, 3000, 64, 0.9), (1, 1100003, 7, 128, 1), (2000, 600, 40, 8, 0.95)])
+def test_slots_past_a_million(n, most, context, page, share):
+    """More slots than the workgroups take at once, not a multiple of four; pages that run out among the last."""
+    rng = np.random.default_rng(n + most)
+    lens, counts, table, free, blocks, n_slots = slots_case(rng, n, most, context, page, share, spare=3)
+    assert n_slots > 1 << 20
+    check_slots(lens, counts if n > 1 else np.array([most], np.int32), table, page, blocks, free if n > 1 else np.arange(blocks, dtype=np.int32)[::-1].copy(), 0, n_slots)
+
+
 # ---------------------------------------------------------------- rows into the cache
 def paged(rng, blocks, heads, page, dim, order):
     """A cache tensor (blocks, heads, page, dim) whose axes lie in memory as `order` says."""
@@ -176,6 +185,54 @@ CASES = [
 def test_attention(lens, counts, heads, kv_heads, dim, page):
     rng = np.random.default_rng(sum(lens) + dim)
     check_tree(tree_case(rng, lens, counts, heads, kv_heads, dim, page, [(0, 1, 2), (0, 2, 1), (1, 0, 2)][dim % 3]))
+
+
+# Every kernel of the attention, in one span and in several (test_serve_host.py asks the library which kernels these are):
+# (head size, key heads, query heads a key head, drafted tokens of the largest request, context of the largest)
+FORMS = [(dim, kv, group, tokens, context) for dim in (40, 64, 72, 96, 128, 160, 192, 200, 256) for context in (77, 1500)
+         for kv, group, tokens in ((3, 1, 1), (2, 1, 20), (1, 4, 8), (2, 1, 50), (2, 2, 50), (2, 4, 50))]
+
+
+def form_case(dim, kv, group, tokens, context):
+    """Three requests: the largest; one that has no context and whose first token sees nothing; a short one."""
+    rng = np.random.default_rng(dim * 1000 + kv * group * tokens + context)
+    c = tree_case(rng, [context, 0, 33], [tokens, max(1, tokens // 3), min(tokens, 2)], kv * group, kv, dim, (16, 1, 64)[(dim // 8) % 3], [(0, 1, 2), (0, 2, 1), (1, 0, 2)][group % 3])
+    c["mask"][tokens] = 0
+    return c
+
+
+@pytest.mark.parametrize("dim,kv,group,tokens,context", FORMS)
+def test_every_form_of_the_attention(dim, kv, group, tokens, context):
+    c = form_case(dim, kv, group, tokens, context)
+    check_tree(c)
+    assert (c["out"][tokens] == 0).all()
+    if tokens > 1:                                        # the last token of a tree is nobody's ancestor
+        want, bound = want_tree(c)
+        c["k"][tokens - 1], c["v"][tokens - 1] = float("nan"), float("inf")
+        others = np.arange(int(c["cu"][-1])) != tokens - 1
+        R.close(run_tree(c)[:len(others)][others], want[:len(others)][others], bound[:len(others)][others])
+
+
+@pytest.mark.parametrize("dim,tokens,context", [(128, 1, 2000), (128, 50, 900), (256, 1, 700), (192, 20, 1200), (64, 1, 3000)])
+def test_captured_attention_of_large_tiles(dim, tokens, context):
+    torch = G.torch_mod()
+    c = form_case(dim, 2, 1, tokens, context)
+    table, lens, cu, mask = dev(c["table"]), dev(c["lens"]), dev(c["cu"]), dev(c["mask"])
+    step = lambda: egt.tree_attention(c["q"], c["k"], c["v"], c["k_cache"], c["v_cache"], table, lens, cu, mask, c["out"], c["scale"], c["max_tokens"], c["ws"])  # noqa: E731
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        lens.copy_(torch.tensor([[context, 0, 33], [5, 1, 0], [context // 2, context, context - 1], [context, 31, 32]][k], dtype=torch.int32))
+        step()
+        torch.cuda.synchronize()
+        want = c["out"].clone()
+        c["out"].fill_(3)
+        c["ws"].fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        used = int(c["cu"][-1])
+        assert torch.equal(c["out"][:used], want[:used]) and bool((c["out"][used:] == 3).all())
 
 
 def test_attention_over_a_long_context():
@@ -389,6 +446,20 @@ def test_adapters_of_many_tokens_and_rows(rows, rank, pad):
     index = rng.integers(-1, 65, 64)                      # none, one past the last, and tokens that share one
     index[40:60] = 7
     c = lora_case(rng, 64, 64, rows, rank, 64, index.tolist(), pad=pad)
+    check_lora(c)
+    check_lora(c, base=False)
+
+
+# Every kernel of the adapters' second product (test_serve_host.py asks the library), with rows that do not fill the last workgroup
+ADAPTER_FORMS = [(rows, rank, pad) for rank in (16, 32, 40, 64, 72, 128) for rows, pad in ((60, 0), (4100, 0), (4100, 4), (2100, 0), (2099, 1))]
+
+
+@pytest.mark.parametrize("rows,rank,pad", ADAPTER_FORMS)
+def test_every_form_of_the_adapters(rows, rank, pad):
+    rng = np.random.default_rng(rows + rank)
+    index = rng.integers(-1, 65, 64)
+    index[40:60] = 7
+    c = lora_case(rng, 64, 72, rows, rank, 64, index.tolist(), pad=pad)
     check_lora(c)
     check_lora(c, base=False)
 

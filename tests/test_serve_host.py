@@ -1,6 +1,7 @@
 """The operators beside the products without a GPU: what they refuse, what their structures look like, their references."""
 import ctypes as C
 import os
+import re
 import shutil
 import subprocess
 
@@ -253,12 +254,25 @@ for heads, dim, n in ((1, 8, 1), (8, 128, (1 << 24) - 1), (1 << 20, 256, 5), (1 
     b = B.AppendBatch(k=P, v=P, slots=P, k_row=128, k_head=64, v_row=128, v_head=64, n=n, n_rows=n)
     print("case append", heads, dim, flush=True)
     print("status", L.egt_kv_append(C.byref(b), C.byref(c), None), flush=True)
+for dim, kv, group, tokens, context in {forms!r}:
+    for page in (1, 16, 64):
+        table = -(-context // page) + 1
+        c = B.KvCache(k=P, v=P, blocks=8, heads=kv, page=page, dim=dim, k_block=8, k_head=8, k_token=8, v_block=8, v_head=8, v_token=8)
+        b = B.TreeBatch(q=P, k=P, v=P, out=P, q_row=8, q_head=8, k_row=8, k_head=8, v_row=8, v_head=8, out_row=8, out_head=8, block_table=P, lens=P, cu_tokens=P, mask=P,
+                        ld_table=table, requests=3, tokens=3 * tokens, heads=kv * group, max_tokens=tokens, table_blocks=table, scale=1.0)
+        print("case form", dim, context, flush=True)
+        print("status", L.egt_tree_attention(C.byref(b), C.byref(c), P, 1 << 40, None), flush=True)
+for rows, rank, pad in {adapters!r}:
+    b = B.LoraBatch(X=P, A=P, B=P, base=P, Y=P, index=P, scale=P, ldx=72, ldbase=rows + pad, ldy=rows + pad, a_stride=512, b_stride=800, M=64, cols=72, rows=rows, rank=rank, adapters=64)
+    print("case adapter", rows, rank, flush=True)
+    print("status", L.egt_lora_smallm(C.byref(b), P, 1 << 30, None), flush=True)
 """
 
 
 @pytest.fixture(scope="module")
 def other_launches(tmp_path_factory):
     """[(case, [(kernel, grid x, grid y, threads, LDS bytes)])]: what runs of the calls above, as a stand-in for the runtime's launch sees it."""
+    import test_gpu_serve as on_the_gpu
     import test_kernel_routes as routes
     cc = shutil.which("gcc")
     if not cc:
@@ -267,7 +281,8 @@ def other_launches(tmp_path_factory):
     (d / "launch.c").write_text(routes.STAND_IN)
     subprocess.run([cc, "-shared", "-fPIC", "-O1", str(d / "launch.c"), "-o", str(d / "launch.so")], check=True)
     env = {**os.environ, "LD_PRELOAD": " ".join(v for v in (str(d / "launch.so"), os.environ.get("LD_PRELOAD", "")) if v)}
-    out = subprocess.run([os.sys.executable, "-c", OTHER_LAUNCHES.replace("{root!r}", repr(ROOT))], capture_output=True, text=True, env=env, timeout=120)
+    script = OTHER_LAUNCHES.replace("{root!r}", repr(ROOT)).replace("{forms!r}", repr(on_the_gpu.FORMS)).replace("{adapters!r}", repr(on_the_gpu.ADAPTER_FORMS))
+    out = subprocess.run([os.sys.executable, "-c", script], capture_output=True, text=True, env=env, timeout=120)
     assert out.returncode == 0, (out.stdout[-300:], out.stderr[-2000:])
     seen = []
     for line in out.stdout.splitlines():
@@ -291,7 +306,7 @@ def test_waves_of_the_slot_maps_have_lds_of_their_own(other_launches):
 def test_launches_of_adapters_and_cache_writes(other_launches):
     """A grid that a launch takes (less than 2^32 threads), or EGT_ERR_UNSUPPORTED and no launch; a token's pieces are counted in 31 bits."""
     kernels = set()
-    for (what, *sizes, status), launches in (c for c in other_launches if c[0][0] != "slots"):
+    for (what, *sizes, status), launches in (c for c in other_launches if c[0][0] in ("lora", "append")):
         sizes = [int(v) for v in sizes]
         fits = sizes[0] <= (1 << 30) - 64 if what == "lora" else sizes[0] * (sizes[1] // 8) <= 1 << 30
         assert status == (0 if fits else UNSUPPORTED) and len(launches) == ((2 if what == "lora" else 1) if fits else 0), (what, sizes)
@@ -299,6 +314,24 @@ def test_launches_of_adapters_and_cache_writes(other_launches):
             assert x * threads < 1 << 32 and y <= 65535, (what, sizes, name)
             kernels.add(name)
     assert len([k for k in kernels if "k_lora_expand" in k]) == 11
+
+
+def test_the_gpu_tests_reach_every_kernel(other_launches):
+    """What the library launches for the cases of the tests on the GPU: every form of the attention, in one span and in several, and
+    every form of the adapters' second product."""
+    def names(launches):
+        text = subprocess.run(["c++filt"], input="\n".join(l[0] for l in launches), capture_output=True, text=True).stdout
+        return set(re.findall(r"k_\w+<[^>]*>|k_tree_join", text))
+    one, several, adapters = set(), set(), set()
+    for (what, *rest), launches in other_launches:
+        if what in ("form", "adapter"):
+            assert rest[-1] == 0
+            found = names(launches)
+            if what == "adapter":
+                adapters |= {k for k in found if "expand" in k}
+            else:
+                (several if "k_tree_join" in found else one).update(k for k in found if k != "k_tree_join")
+    assert len(one) == len(several) == 23 and one == several and len(adapters) == 11
 
 
 BIG = 1 << 30
