@@ -791,7 +791,8 @@ def tree_attention(q, k, v, k_cache, v_cache, block_table, lens, cu_tokens, mask
                    workspace=None, stream=None) -> None:
     """Attention of drafted tokens over their requests' cached context and over those of their own request that mask
     (int64, one bit a token) shows: q, out (N, heads, dim), k, v (N, key heads, dim), caches as for `kv_append`, block_table
-    (R, W), lens (R,), cu_tokens (R + 1,) int32.  `workspace`: a device tensor of tree_attention_ws_bytes bytes."""
+    (R, W), lens (R,), cu_tokens (R + 1,) int32.  `workspace`: a device tensor of tree_attention_ws_bytes bytes (a call without
+    one is refused)."""
     (_call or _native()).tree_attention(False, q, k, v, k_cache, v_cache, block_table, lens, cu_tokens, mask, out, scale, max_tokens, workspace, stream)
 
 

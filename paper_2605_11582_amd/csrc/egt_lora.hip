@@ -270,8 +270,11 @@ __global__ __launch_bounds__(256, 2) void k_lora_expand(egt_lora_batch b, const 
 
 template <int RC>
 hipError_t launch_expand(const egt_lora_batch &b, const float *part, int slices, hipStream_t stream) {
-  // row tiles a wave: more where there are plenty of rows if every token has an adapter of its own (the workgroups of tokens that
-  // another one speaks for are launched too)
+  // Row tiles a wave: more where there are plenty of rows if every token has an adapter of its own (the workgroups of tokens that
+  // another one speaks for are launched too).  us of both kernels, 1024 columns, ranks 32 / 64 / 128, one tile against four: 512 groups
+  // 8.0 / 10.0 / 16.2 against 8.4 / 10.3 / 16.2, 1024 groups 9.2 / 12.8 / 20.2 against 8.5 / 11.4 / 18.0, 2048 groups 13.1 / 17.8 / 26.8
+  // against 9.8 / 14.2 / 21.3; four against eight, ranks 32 / 64: 3008 groups 11.9 / 16.0 against 11.5 / 16.2, 4096 groups 12.6 / 19.5
+  // against 11.9 / 16.9, 11008 groups 20.6 / 33.3 against 17.7 / 30.2 (rank 128 has no registers for eight).
   const int64_t groups = (int64_t)((b.rows + 63) / 64) * std::min(b.M, b.adapters);
   const bool whole = b.rows % 4 == 0 && b.ldy % 4 == 0 && ((uintptr_t)b.Y & 7) == 0 && (!b.base || (b.ldbase % 4 == 0 && ((uintptr_t)b.base & 7) == 0));
   if (!whole) return launch(k_lora_expand<RC, 1, false>, dim3((b.rows + 63) / 64, b.M), dim3(256), 0, stream, b, part, slices);

@@ -309,9 +309,12 @@ egt_status egt_logits_rules(const egt_rules_batch *b, void *stream) {
                         (const void *)b->repetition, (const void *)b->frequency, (const void *)b->presence, (const void *)b->bias_ids, (const void *)b->bias,
                         (const void *)b->allowed, (const void *)b->allowed_row})
     if ((uintptr_t)p & 3) return EGT_ERR_BUFFER;
-  // Slices of 4096 ids count a history in fewer workgroups; where rows are few, slices of 1024 have the whole chip at work.  Rows of one
-  // request share a count: as many together as a request has on average, as long as there are 2048 workgroups (128 rows of
-  // 128000 ids, 72 of them used: 1024 workgroups 19.1 us, 2048 16.0, 4096 18.8).
+  // Slices of 4096 ids count a history in fewer workgroups; where rows are few, slices of 1024 have the whole chip at work (us, slices of
+  // 1024 against 4096, FP16, histories of 2048 ids, a token a request: 128 workgroups of 4096 ids 6.3 / 6.8, 256 7.9 / 7.0,
+  // 512 12.3 / 7.8, 1024 21.0 / 10.4; FP32 6.7 / 7.0, 8.1 / 7.2, 13.0 / 9.0, 23.0 / 14.8).  Rows of one request share a count: as many
+  // together as a request has on average, as long as there are 2048 workgroups (us with 1024, 2048 and 4096: sixteen requests, 72 of 128
+  // rows used, 128000 ids 20.6, 19.9, 21.7; all 128 rows 22.3, 24.8, 31.6; 512 rows of eight requests 77, 75, 80; 256 rows of 64
+  // requests, 32003 ids 16.7, 20.2, 20.1).
   const bool large = (int64_t)b->tokens * ((b->vocab + 4095) / 4096) >= 512;
   const int slices = large ? (b->vocab + 4095) / 4096 : (b->vocab + 1023) / 1024;
   const int64_t each = std::min<int64_t>((int64_t)b->tokens * slices / 2048, (b->tokens + b->requests - 1) / b->requests);

@@ -15,10 +15,11 @@
 //                  V^T comes out of LDS by the transposing read; the sum of p is one more product, with ones.
 //
 // What bounds it: with up to 64 rows a key head the cache's bytes (16 rows over 131072 keys, 8 heads of 128: 107 us, 5.0 TB/s;
-// 64 rows 116 us), above that the steps themselves, of which one wave a SIMD can hide little: 256 rows 183 us, 2.9 TB/s and
-// 0.73 PFLOP/s, matrix units busy 38 % of the time and vector units 46 %.  A wave of two row tiles spends, of 2500 cycles a step,
+// 64 rows 116 us), above that the steps themselves, of which one wave a SIMD can hide little: 256 rows 187 us (184 to 193 from card to
+// card, the join's 10 among them), 2.9 TB/s and 0.74 PFLOP/s, matrix units busy 40 % of the first kernel's time and vector units 45 %; its
+// kernel keeps 68 bytes a lane in scratch.  A wave of two row tiles spends, of 2500 cycles a step,
 // 345 on staging, 500 on addresses and requests, 610 on scores (256 of them products), 390 on weights and 555 on sums (288).  Short
-// contexts are bound by a launch and the chain lengths - page numbers - keys, 8.4 us, and a launch more where there are several spans.
+// contexts are bound by a launch and the chain lengths - page numbers - keys, 8 to 10 us, and a launch more where there are several spans.
 #include "egt_mfma_common.h"
 #include "egt_serve.h"
 
@@ -94,8 +95,11 @@ __global__ __launch_bounds__(64 * waves_of(DC, WR), DC > 4 && WR < 8 ? 1 : 2) vo
   const int wr = wave % WR, wk = wave / WR, dim = a.c.dim;
   const int r = blockIdx.z, kh = blockIdx.y / a.row_blocks, rb = blockIdx.y % a.row_blocks;
   const int t0 = a.b.cu_tokens[r], t1 = a.b.cu_tokens[r + 1], len = a.b.lens[r];
-  // The arguments are five lines of memory: asked for together, not one behind the other as they come up (seven requests of up
-  // to 33 tokens and 3001 keys 20.9 -> 19.4 us); not where registers are short (256 rows over 131072 keys 186 -> 194 us).
+  // The arguments are five lines of memory: asked for together, not one behind the other as they come up (us, so against left to
+  // the compiler: seven requests of up to 31 tokens and 3000 keys, heads of 80, 22.8 / 24.1; one token over 777 keys, heads of 64, 128 and 192,
+  // 10.4 / 10.5, 14.2 / 14.4 and 17.0 / 17.3; 256 rows over 32768 keys, heads of 96, 59.0 / 60.5; 80 rows of them, eight requests, 37.4 / 36.2).
+  // Not where registers are short (heads of 128: 256 rows over 131072 keys 204 / 196, 80 rows, sixteen requests, 52.4 / 51.5; heads
+  // of 200 to 256, one wave a SIMD: no difference).
   if constexpr (NR * DC < 8)
     asm volatile("" ::"s"(a.b.q), "s"(a.b.k_row), "s"(a.b.mask), "s"(a.b.requests), "s"(a.c.k), "s"(a.c.k_head), "s"(a.part), "s"(a.scale2));
   const int state = request_state(a, t0, t1, len);
@@ -536,7 +540,7 @@ Shape shape_of(const egt_tree_batch &b, const egt_kv_cache &c) {
   Shape s;
   const int rows = b.max_tokens * (b.heads / c.heads);
   // Two row tiles a wave from 65 rows on (up to 128 rows, us, two tiles of four waves against one of eight: sixteen requests of up to 80 rows
-  // 52.8 / 53.9, 128 rows over 131072 keys 151 / 185); wider heads have no registers for them.
+  // 52.8 / 53.9, 128 rows over 131072 keys 151 / 185 when both were there, 130 to 140 now); wider heads have no registers for them.
   s.nr = rows <= 64 || c.dim > 128 ? 1 : 2;
   s.wr = 1;
   while (s.wr < 8 && rows > 16 * s.nr * s.wr) s.wr *= 2;
